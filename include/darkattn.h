@@ -218,6 +218,89 @@ size_t darkattn_static_scratch_needed(darkattn_plan_t plan);
 darkattn_status_t darkattn_forward_static(darkattn_plan_t plan, const void *Q, const void *K, const void *V,
                                           const void *M, const void *W, void *O, void *cuda_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Linear attention with a decay per head.
+ *
+ * The running state of causal linear attention (Section 2's ordering, one token at a time) grows with every token; a
+ * decay lambda_n = exp(log_decay[n]) <= 1 per key/value head n lets it forget. For every batch b and query head h,
+ * n = h / (H / H_kv), on queries and keys that the caller has mapped as it likes (to features or not at all):
+ *
+ *   S_t = lambda_n S_{t-1} + k_t v_t^T,     o_t = scale q_t^T S_t,     S_0 = S_in (or zero)
+ *   O   = scale ( [lambda^(i-j) q_i.k_j for j <= i, else 0] V + [lambda^i] Q S_in )         (i, j = 1 .. N)
+ *
+ * There is no normaliser: append a column of ones to V for one. The decays are constants of the model, no gradient
+ * is formed for them; log_decay = -infinity (lambda = 0: the token itself alone) is allowed, and values above 0 are not
+ * refused but overflow like the formula does.
+ *
+ *   Q, dQ       [B, H, N, d]       desc.dtype          K, dK   [B, H_kv, N, d]    desc.dtype
+ *   O, dO       [B, H, N, dv]      desc.dtype          V, dV   [B, H_kv, N, dv]   desc.dtype
+ *   S_*, dS_*   [B, H_kv, d, dv]   float32             log_decay  [H_kv]          float32
+ *   lengths     [B]                int32, or NULL: all N. Sequence b has lengths[b] tokens (taken into 0 .. N), the rows behind
+ *                                  them are padding: never used, whatever they hold. Rows of O behind the end are left as
+ *                                  they were, those of dQ, dK and dV are set to zero.
+ *
+ * Conventions as at the top of this file (contiguous, 16-byte aligned - log_decay, lengths and slots 4 -, caller-owned,
+ * asynchronous on the stream, nothing allocated). Inputs have to be finite: what is not spreads to its whole chunk. */
+typedef struct {
+    int32_t B, H, N;      /* batch, query heads, (padded) sequence length; all >= 1, B H <= 65535             */
+    int32_t d;            /* query/key width, 1 .. 512                                                          */
+    int32_t dv;           /* value width, 1 .. 512; 0 means d                                                   */
+    int32_t dtype;        /* darkattn_dtype_t                                                                   */
+    int32_t H_kv;         /* key/value heads, divides H; 0 means H. One state and one decay each                */
+    int32_t path;         /* AUTO, SIMT (FP32 arithmetic, any shape) or TENSOR (tcgen05; bf16, d and dv multiples of 8, at
+                             most 128; DARKATTN_ERR_UNSUPPORTED elsewhere)                                      */
+    float   scale;        /* 0 means 1/sqrt(d)                                                                  */
+} darkattn_decay_desc_t;
+
+typedef struct darkattn_decay_plan_s *darkattn_decay_plan_t;
+
+darkattn_status_t darkattn_decay_plan(const darkattn_decay_desc_t *desc, darkattn_decay_plan_t *out);   /* host only */
+size_t darkattn_decay_workspace_bytes(darkattn_decay_plan_t plan);       /* for forward and backward alike */
+int32_t darkattn_decay_plan_path(darkattn_decay_plan_t plan);
+void darkattn_decay_destroy(darkattn_decay_plan_t plan);
+
+/* The chunked form: a whole (batch of) prompt(s). S_in: the state before the first token, or NULL. S_out: receives the state
+ * behind the last token of each sequence, or NULL; must not overlap S_in. Sequences are cut into segments where there are too
+ * few heads for the GPU; the states between them live in the workspace.                                      */
+darkattn_status_t darkattn_decay_forward(darkattn_decay_plan_t plan, const void *Q, const void *K, const void *V, const float *log_decay,
+                                         const int32_t *lengths /* nullable */, const float *S_in /* nullable */, void *O,
+                                         float *S_out /* nullable */, void *workspace, void *cuda_stream);
+
+/* Gradients of L = sum(dO .* O) + sum(dS_out .* S_out): dS_out is the gradient with respect to the state behind the last
+ * token (NULL: zero), dS_in receives the one with respect to the state before the first (NULL: not wanted; must overlap
+ * neither dS_out nor S_in). dK, dV and dS_in sum over the query heads of a group. Needs nothing from the forward pass.   */
+darkattn_status_t darkattn_decay_backward(darkattn_decay_plan_t plan, const void *Q, const void *K, const void *V, const float *log_decay,
+                                          const int32_t *lengths /* nullable */, const float *S_in /* nullable */, const void *dO,
+                                          const float *dS_out /* nullable */, void *dQ, void *dK, void *dV, float *dS_in /* nullable */,
+                                          void *workspace, void *cuda_stream);
+
+/* The recurrent form: one token of each sequence. q [B, H, d], k [B, H_kv, d], v [B, H_kv, dv], o [B, H, dv]; N is not used.
+ * S [n_slots, H_kv, d, dv], a pool of states, is updated in place: sequence b's state is S[slots[b]], or S[b] where slots (int32
+ * [B]) is NULL. A row whose slot is outside 0 .. n_slots - 1 is padding, and so is one whose slot an earlier row has named:
+ * neither its output nor a state is touched. No workspace; one launch. DARKATTN_ERR_UNSUPPORTED where the queries of a group
+ * (H / H_kv rows of d) do not fit a block's shared memory: (H / H_kv) (d + 256) + d must not be above 51200.             */
+darkattn_status_t darkattn_decay_step(darkattn_decay_plan_t plan, const void *q, const void *k, const void *v, const float *log_decay, float *S,
+                                      const int32_t *slots /* nullable */, int32_t n_slots, void *o, void *cuda_stream);
+
+/* As darkattn_last_device_status, for the workspace of the last decay_forward or decay_backward.                 */
+darkattn_status_t darkattn_decay_last_device_status(darkattn_decay_plan_t plan, const void *workspace, void *cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * A cache of running states in 8 bits: states of finished prompts kept for sequences that continue them (those of
+ * darkattn_decay_forward, or S and z of darkattn_decode_step). A row of cols numbers is kept as cols codes and one scale:
+ * scale = max |x| / top in float32, code = x / scale rounded to nearest (ties to even) from the exact quotient.
+ *   I8   : signed integers, top = 127; off by at most max |x| / 254
+ *   E4M3 : 8-bit floating point, top = 448; off by at most 2^-4 of the value, or max |x| / 458752 where that is more
+ * A row that holds an infinity or NaN is read back as NaN throughout.
+ *   S [B, rows, cols] float32;  codes [n_slots, rows, cols] one byte each;  scales [n_slots, rows] float32
+ * (rows: heads times the state's rows). Sequence b is kept in slot slots[b] (b where slots is NULL). Padding as in
+ * darkattn_decay_step: rows whose slot is out of range, and for the store those whose slot an earlier row has named.    */
+typedef enum { DARKATTN_STATE_I8 = 0, DARKATTN_STATE_E4M3 = 1 } darkattn_state_format_t;
+darkattn_status_t darkattn_state_store(int32_t B, int32_t rows, int32_t cols, const float *S, const int32_t *slots /* nullable */,
+                                       int32_t n_slots, int32_t format, void *codes, float *scales, void *cuda_stream);
+darkattn_status_t darkattn_state_load(int32_t B, int32_t rows, int32_t cols, const void *codes, const float *scales,
+                                      const int32_t *slots /* nullable */, int32_t n_slots, int32_t format, float *S, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libdarkattn.so")
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_NONFINITE = range(7)
 F32, BF16 = 0, 1
 PATH_AUTO, PATH_SIMT, PATH_TENSOR = 0, 1, 2
+STATE_I8, STATE_E4M3 = 0, 1
 
 EXPORTS = [
     "darkattn_plan", "darkattn_workspace_bytes", "darkattn_workspace_bytes_with_saved", "darkattn_saved_bytes", "darkattn_plan_path",
@@ -25,6 +26,9 @@ EXPORTS = [
     "darkattn_destroy", "darkattn_status_string", "darkattn_last_cuda_error", "darkattn_measure_alu_peak",
     "darkattn_static_scratch_needed", "darkattn_forward_static",
     "darkattn_backward_dw", "darkattn_decode_step", "darkattn_selftest_wait_limit",
+    "darkattn_decay_plan", "darkattn_decay_workspace_bytes", "darkattn_decay_plan_path", "darkattn_decay_destroy",
+    "darkattn_decay_forward", "darkattn_decay_backward", "darkattn_decay_step", "darkattn_decay_last_device_status",
+    "darkattn_state_store", "darkattn_state_load",
 ]
 # instruments of the benchmark, in a library of their own (include/darkattn_bench.h)
 BENCH_EXPORTS = ["darkattn_plan_launches", "darkattn_plan_rows_summed", "darkattn_kernel_timing", "darkattn_kernel_times", "darkattn_measure_mma_cycles"]
@@ -36,6 +40,11 @@ class Desc(ctypes.Structure):
                 ("r", ctypes.c_int32), ("m", ctypes.c_int32), ("dv", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("causal", ctypes.c_int32), ("chunk", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("w_per_head", ctypes.c_int32), ("path", ctypes.c_int32), ("H_kv", ctypes.c_int32)]
+
+
+class DecayDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("N", ctypes.c_int32), ("d", ctypes.c_int32), ("dv", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("path", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -78,6 +87,26 @@ lib.darkattn_static_scratch_needed.argtypes = [_vp]
 lib.darkattn_static_scratch_needed.restype = ctypes.c_size_t
 lib.darkattn_forward_static.argtypes = [_vp] * 8
 lib.darkattn_forward_static.restype = ctypes.c_int
+lib.darkattn_decay_plan.argtypes = [ctypes.POINTER(DecayDesc), ctypes.POINTER(_vp)]
+lib.darkattn_decay_plan.restype = ctypes.c_int
+lib.darkattn_decay_workspace_bytes.argtypes = [_vp]
+lib.darkattn_decay_workspace_bytes.restype = ctypes.c_size_t
+lib.darkattn_decay_plan_path.argtypes = [_vp]
+lib.darkattn_decay_plan_path.restype = ctypes.c_int32
+lib.darkattn_decay_destroy.argtypes = [_vp]
+lib.darkattn_decay_destroy.restype = None
+lib.darkattn_decay_forward.argtypes = [_vp] * 11
+lib.darkattn_decay_forward.restype = ctypes.c_int
+lib.darkattn_decay_backward.argtypes = [_vp] * 15
+lib.darkattn_decay_backward.restype = ctypes.c_int
+lib.darkattn_decay_step.argtypes = [_vp] * 7 + [ctypes.c_int32, _vp, _vp]
+lib.darkattn_decay_step.restype = ctypes.c_int
+lib.darkattn_decay_last_device_status.argtypes = [_vp, _vp, _vp]
+lib.darkattn_decay_last_device_status.restype = ctypes.c_int
+lib.darkattn_state_store.argtypes = [ctypes.c_int32] * 3 + [_vp, _vp, ctypes.c_int32, ctypes.c_int32, _vp, _vp, _vp]
+lib.darkattn_state_store.restype = ctypes.c_int
+lib.darkattn_state_load.argtypes = [ctypes.c_int32] * 3 + [_vp, _vp, _vp, ctypes.c_int32, ctypes.c_int32, _vp, _vp]
+lib.darkattn_state_load.restype = ctypes.c_int
 
 
 BENCH_LIB_PATH = os.path.join(_HERE, "libdarkattn_bench.so")
@@ -278,3 +307,129 @@ def darkattn_forward_static(plan: Plan, Q, K, V, M, W, O, stream=None):
     _check(lib.darkattn_forward_static(plan.handle, _ptr(Q), _ptr(K), _ptr(V), _ptr(M), _ptr(W), _ptr(O),
                                        _stream(stream)), "darkattn_forward_static")
     return O
+
+
+# ---------------------------------------------------------------- attention with a decay per head, 8-bit state cache
+@dataclass
+class DecayPlan:
+    """Owner of a darkattn_decay_plan_t handle."""
+    handle: int
+    desc: DecayDesc
+
+    def __post_init__(self):
+        ds = self.desc
+        self._dt = torch.float32 if ds.dtype == F32 else torch.bfloat16
+        self._q, self._k = (ds.B, ds.H, ds.N, ds.d), (ds.B, ds.H_kv, ds.N, ds.d)
+        self._v, self._o = (ds.B, ds.H_kv, ds.N, ds.dv), (ds.B, ds.H, ds.N, ds.dv)
+        self._s = (ds.B, ds.H_kv, ds.d, ds.dv)
+        self._token = [(ds.B, ds.H, ds.d), (ds.B, ds.H_kv, ds.d), (ds.B, ds.H_kv, ds.dv), (ds.B, ds.H, ds.dv)]
+
+    @property
+    def workspace_bytes(self) -> int:
+        return int(lib.darkattn_decay_workspace_bytes(self.handle))
+
+    @property
+    def path(self) -> int:
+        return int(lib.darkattn_decay_plan_path(self.handle))
+
+    def alloc_workspace(self, device="cuda") -> torch.Tensor:
+        return torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)
+
+    def destroy(self):
+        if self.handle:
+            lib.darkattn_decay_destroy(self.handle)
+            self.handle = 0
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def darkattn_decay_plan(B, H, N, d, *, dv=0, dtype=BF16, H_kv=0, path=PATH_AUTO, scale=0.0) -> DecayPlan:
+    desc = DecayDesc(B, H, N, d, dv, dtype, H_kv, path, float(scale))
+    h = _vp()
+    _check(lib.darkattn_decay_plan(ctypes.byref(desc), ctypes.byref(h)), "darkattn_decay_plan")
+    desc.dv, desc.H_kv = dv or d, H_kv or H
+    return DecayPlan(h.value, desc)
+
+
+def _arg(t, name, shape, dtype, device=None):
+    """A tensor's address, after the checks that keep the kernels inside of it."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}: {dtype} {tuple(shape)} is expected")
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} has to be a contiguous CUDA tensor")
+    if t.get_device() != (torch.cuda.current_device() if device is None else device):
+        raise ValueError(f"{name} is on another device than the current one")
+    return t.data_ptr()
+
+
+def _workspace(plan, t, device):
+    if t.numel() * t.element_size() < plan.workspace_bytes:
+        raise ValueError(f"workspace has {t.numel() * t.element_size()} bytes: {plan.workspace_bytes} are needed")
+    return _arg(t, "workspace", t.shape, t.dtype, device)
+
+
+def darkattn_decay_forward(plan: DecayPlan, Q, K, V, log_decay, O, workspace, lengths=None, S_in=None, S_out=None, stream=None):
+    p, dt, dev = plan, plan._dt, torch.cuda.current_device()
+    _check(lib.darkattn_decay_forward(p.handle, _arg(Q, "Q", p._q, dt, dev), _arg(K, "K", p._k, dt, dev), _arg(V, "V", p._v, dt, dev),
+                                      _arg(log_decay, "log_decay", (p.desc.H_kv,), torch.float32, dev),
+                                      _arg(lengths, "lengths", (p.desc.B,), torch.int32, dev), _arg(S_in, "S_in", p._s, torch.float32, dev),
+                                      _arg(O, "O", p._o, dt, dev), _arg(S_out, "S_out", p._s, torch.float32, dev), _workspace(p, workspace, dev),
+                                      _stream(stream)), "darkattn_decay_forward")
+    return O
+
+
+def darkattn_decay_backward(plan: DecayPlan, Q, K, V, log_decay, dO, dQ, dK, dV, workspace, lengths=None, S_in=None, dS_out=None, dS_in=None,
+                            stream=None):
+    p, dt, dev = plan, plan._dt, torch.cuda.current_device()
+    _check(lib.darkattn_decay_backward(p.handle, _arg(Q, "Q", p._q, dt, dev), _arg(K, "K", p._k, dt, dev), _arg(V, "V", p._v, dt, dev),
+                                       _arg(log_decay, "log_decay", (p.desc.H_kv,), torch.float32, dev),
+                                       _arg(lengths, "lengths", (p.desc.B,), torch.int32, dev), _arg(S_in, "S_in", p._s, torch.float32, dev),
+                                       _arg(dO, "dO", p._o, dt, dev), _arg(dS_out, "dS_out", p._s, torch.float32, dev), _arg(dQ, "dQ", p._q, dt, dev),
+                                       _arg(dK, "dK", p._k, dt, dev), _arg(dV, "dV", p._v, dt, dev), _arg(dS_in, "dS_in", p._s, torch.float32, dev),
+                                       _workspace(p, workspace, dev), _stream(stream)), "darkattn_decay_backward")
+    return dQ, dK, dV
+
+
+def darkattn_decay_step(plan: DecayPlan, q, k, v, log_decay, S, o, slots=None, stream=None):
+    """One token of each sequence: the pool of states S [n_slots, H_kv, d, dv] is updated in place, o receives the output."""
+    p, dt, dev = plan, plan._dt, torch.cuda.current_device()
+    qs, ks, vs, os_ = p._token
+    _check(lib.darkattn_decay_step(p.handle, _arg(q, "q", qs, dt, dev), _arg(k, "k", ks, dt, dev), _arg(v, "v", vs, dt, dev),
+                                   _arg(log_decay, "log_decay", (p.desc.H_kv,), torch.float32, dev), _arg(S, "S", S.shape[:1] + p._s[1:], torch.float32, dev),
+                                   _arg(slots, "slots", (p.desc.B,), torch.int32, dev), S.shape[0], _arg(o, "o", os_, dt, dev), _stream(stream)),
+           "darkattn_decay_step")
+    return o
+
+
+def darkattn_decay_last_device_status(plan: DecayPlan, workspace, stream=None) -> int:
+    return int(lib.darkattn_decay_last_device_status(plan.handle, _ptr(workspace), _stream(stream)))
+
+
+def _state_args(S, codes, scales, slots, format):
+    dev = torch.cuda.current_device()
+    if S.dim() < 2 or codes.dim() != S.dim() or codes.element_size() != 1:
+        raise ValueError("S is [B, ..., cols], codes one byte an element [n_slots, ..., cols]")
+    n, cols = codes.shape[0], S.shape[-1]
+    args = (_arg(S, "S", S.shape, torch.float32, dev), _arg(codes, "codes", (n,) + tuple(S.shape[1:]), codes.dtype, dev),
+            _arg(scales, "scales", (n,) + tuple(S.shape[1:-1]), torch.float32, dev), _arg(slots, "slots", S.shape[:1], torch.int32, dev))
+    B = S.shape[0]
+    return (B, S.numel() // max(B * cols, 1), cols, n, int(format)) + args
+
+
+def darkattn_state_store(S, codes, scales, slots=None, format=STATE_I8, stream=None):
+    """Rows of S [B, ..., cols] into the 8-bit cache codes [n_slots, ..., cols], scales [n_slots, ...]."""
+    B, rows, cols, n, fmt, S_, c_, sc_, sl_ = _state_args(S, codes, scales, slots, format)
+    _check(lib.darkattn_state_store(B, rows, cols, S_, sl_, n, fmt, c_, sc_, _stream(stream)), "darkattn_state_store")
+
+
+def darkattn_state_load(codes, scales, S, slots=None, format=STATE_I8, stream=None):
+    """Rows of the 8-bit cache back into S [B, ..., cols]."""
+    B, rows, cols, n, fmt, S_, c_, sc_, sl_ = _state_args(S, codes, scales, slots, format)
+    _check(lib.darkattn_state_load(B, rows, cols, c_, sc_, sl_, n, fmt, S_, _stream(stream)), "darkattn_state_load")
+    return S

@@ -1,0 +1,95 @@
+// Attention with a decay per head: what its kernels and its host side share.
+//
+// The forward pass and the three gradients are one operator on rows x, y (a wide) and z (c wide) of a sequence,
+//     out_i = p_mul sum_j lambda^|i-j| (x_i . y_j) z_j + row_mul lambda^(distance of i to the boundary) x_i S,
+// j running over i and what lies before it in the pass's direction, S the state at the boundary the pass enters by:
+//     O : (Q, K, V)  forwards      S = sum_j lambda^(..) k_j v_j^T
+//     dQ: (dO, V, K) forwards      S^T
+//     dK: (V, dO, Q) backwards     R^T,  R = sum_i lambda^(..) scale q_i do_i^T, the gradient of the state
+//     dV: (K, Q, dO) backwards     R
+// It is evaluated in chunks: masked products inside a chunk, the state between chunks. In a chunk of L rows, row r lies r + 1 steps
+// behind the boundary before it and L - 1 - r before the one after it, so a pass forwards reads the state by lambda^(r+1) and adds
+// row r to it by lambda^(L-1-r), a pass backwards the other way round, and either multiplies the state by lambda^L: every
+// power of lambda is one of 0 .. L, never a quotient, so that no decay is too strong.
+#pragma once
+
+#include "common.cuh"
+
+namespace darkattn {
+
+struct DecayPass {
+    const void *X, *Y, *Z;      // [B, HX, N, a], [B, HY, N, a], [B, HY, N, c]
+    void *O;                    // [B, HX, N, c]
+    const float *S_in;          // state the pass enters by, [B, Hkv, d, dv]; null: zero
+    float *S_out;               // state it leaves by; null: not wanted (always null where trans is set)
+    const float *seg;           // states the segments behind the first enter by, [B * Hkv, nseg - 1, d, dv]
+    int a, c;
+    int HX, HY;                 // heads of X and O, and of Y and Z: where HX > HY consecutive heads of X share one of Y, where
+                                // HY > HX the sum runs over consecutive heads of Y
+    int reverse;                // direction
+    int trans;                  // S is [c, a] in memory
+    float p_mul, row_mul, tok_mul;   // tok_mul: of a token's share of the state
+};
+
+constexpr int kDecayPasses = 3;
+
+struct DecayArgs {
+    DecayPass pass[kDecayPasses];
+    int npass;
+    const float *log_decay;     // [Hkv]
+    const int *lengths;         // [B] or null
+    int B, Hkv, N;
+    int nseg, cps;              // segments of a sequence, chunks of each
+    int *status;
+};
+
+// Segments are counted in the order the pass takes the chunks: its k-th chunk is chunk k forwards, T - 1 - k backwards.
+struct DecaySpan {
+    int n, T;                   // tokens and chunks of this sequence
+    int k0, k1;                 // chunks of this segment, in the pass's order
+};
+template <int C>
+__device__ __forceinline__ DecaySpan decay_span(const DecayArgs &A, int b, int seg)
+{
+    DecaySpan s;
+    s.n = A.N;
+    if (A.lengths) s.n = min(max(A.lengths[b], 0), A.N);
+    s.T = (s.n + C - 1) / C;
+    s.k0 = min(seg * A.cps, s.T);
+    s.k1 = min(s.k0 + A.cps, s.T);
+    return s;
+}
+// lambda^n, right to the last bit or so: the tables are a few numbers per block
+__device__ __forceinline__ float decay_power(float g, int n) { return n == 0 ? 1.f : (float)exp((double)g * (double)n); }
+
+struct darkattn_decay_layout {
+    size_t status, seg[2], bytes;        // seg: states of the segments of a pass forwards, of one backwards
+};
+
+}  // namespace darkattn
+
+struct darkattn_decay_plan_s {
+    darkattn_decay_desc_t desc;
+    int path;
+    struct { int nseg, cps; } fwd, bwd;
+    darkattn::darkattn_decay_layout ws;
+    size_t workspace_bytes;
+};
+
+namespace darkattn {
+
+// FP32 kernels, any shape
+void decay_simt_split(darkattn_decay_plan_s *plan);
+darkattn_status_t decay_simt_run(DecayArgs &A, DecayPass *state_pass, int nstate, int bf16, cudaStream_t st);
+// Adds up the segments' states in place: slot s then holds the state that segment s + 1 enters by.
+cudaError_t decay_scan_segments(const DecayArgs &A, const DecayPass &p, int chunk, cudaStream_t st);
+
+// tcgen05 kernels, bf16
+bool decay_tc_supported(const darkattn_decay_desc_t &ds);
+void decay_tc_split(darkattn_decay_plan_s *plan);
+darkattn_status_t decay_tc_run(DecayArgs &A, DecayPass *state_pass, int nstate, cudaStream_t st);
+
+darkattn_status_t decay_step(const darkattn_decay_plan_s *plan, const void *q, const void *k, const void *v, const float *log_decay,
+                             float *S, const int *slots, int n_slots, void *o, cudaStream_t st);
+
+}  // namespace darkattn
