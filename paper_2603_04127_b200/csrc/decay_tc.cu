@@ -1,6 +1,447 @@
+// Attention with a decay per head on the tensor cores: bf16 rows, chunks of 128, products with fp32 accumulation.
+//
+// One block takes a segment of one head's chunks in the pass's order; a chunk is five products of tcgen05.mma:
+//   A  = X Y^T                       scores; times the decays and rounded to bf16 they go back to tensor memory as P, the left operand of
+//   O  = lambda^(..) (X S) + P Z     the rows out: X S first, its rows scaled in place, P Z accumulated onto it
+//   Bt = Y^T I                       (16 tokens at a time) Y transposed into tensor memory (exact), where each token is a column: its weight is applied there in
+//                                    fp32, and the result goes back as three bf16 parts (together 24 bits), the left operands of
+//   D  = (w Y)^T Z                   what the chunk adds to the state
+// The state itself stays in the registers of 16 warps in fp32, S <- lambda^L S + D; the rows read a copy rounded to bf16 (as P is
+// rounded: half a step of each term, like the rounding of the rows out).
+// Everything moves by TMA, two chunks of X, Y and Z deep; the rows out are staged in the chunk's own tiles.
 #include "decay.cuh"
+#include "tc_common.cuh"
+
 namespace darkattn {
-bool decay_tc_supported(const darkattn_decay_desc_t &) { return false; }
-void decay_tc_split(darkattn_decay_plan_s *) {}
-darkattn_status_t decay_tc_run(DecayArgs &, DecayPass *, int, cudaStream_t) { return DARKATTN_ERR_UNSUPPORTED; }
+namespace {
+using namespace tc;
+
+constexpr int C = 128, kBlock = 576;                     // 16 warps, one that loads and stores, one that issues products
+constexpr uint32_t kA = 0, kB = 128, kO = 256, kD = 384; // columns of tensor memory
+
+struct TcMaps { CUtensorMap x, y, z, o; };
+struct TcArgs { DecayArgs a; TcMaps m[kDecayPasses]; };
+
+enum { FULL0, FULL1, SCORES, YT, INTER, DS, PZ, TMA_BARS, P_READY = TMA_BARS, T_READY, S_READY, O_READ, STAGED, CLEAN, NBARS };
+
+template <int DY, int DZ, bool MAIN>
+struct TcSmem {
+    static constexpr int kX = MAIN ? DY / 64 * 16384 : 0, kY = DY / 64 * 16384, kZ = DZ / 64 * 16384;
+    static constexpr int kStage = kX + kY + kZ;
+    static constexpr int S = 2 * kStage, I = S + (MAIN ? kZ : 0), tok = I + 512, pw = tok + 512, bars = pw + 528, slot = bars + NBARS * 8, total = slot + 16;
+    static_assert(total <= 232448, "shared memory of a block");
+};
+
+// tiles of 64 columns and 128 rows of one head: [heads, N, width]
+__device__ __forceinline__ void load3(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z) : "memory");
 }
+__device__ __forceinline__ void store3(const CUtensorMap *map, const void *src, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z) : "memory");
+}
+// Matrix descriptor of an operand that is not swizzled: blocks of 8 rows of 16 bytes, lbo and sbo bytes apart.
+__device__ __forceinline__ uint64_t plain_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) { return make_sdesc(addr, lbo, sbo) & ~((uint64_t)7 << 61); }
+template <int N> __device__ __forceinline__ void tmem_ld(uint32_t a, uint32_t (&v)[N])
+{
+    if constexpr (N == 32) tmem_ld32(a, v);
+    else tmem_ld16(a, v);
+}
+template <int N> __device__ __forceinline__ void tmem_st(uint32_t a, const uint32_t (&v)[N])
+{
+    if constexpr (N == 32) tmem_st32(a, v);
+    else tmem_st16(a, v);
+}
+__device__ __forceinline__ float f(uint32_t x) { return __uint_as_float(x); }
+
+// Two fp32 numbers as three pairs of bf16 parts; what is left of each is below 2^-25 of it.
+__device__ __forceinline__ void split3(float a, float b, uint32_t &p0, uint32_t &p1, uint32_t &p2)
+{
+    p0 = pack_bf16(a, b);
+    a -= f(p0 << 16); b -= f(p0 & 0xffff0000u);
+    p1 = pack_bf16(a, b);
+    a -= f(p1 << 16); b -= f(p1 & 0xffff0000u);
+    p2 = pack_bf16(a, b);
+}
+
+// MAIN: rows out; otherwise only the state of each of the first nseg - 1 segments, from zero, into pass.seg
+template <int DY, int DZ, bool MAIN>
+__global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_constant__ TcArgs P)
+{
+    using M = TcSmem<DY, DZ, MAIN>;
+    constexpr int W = DZ / 4;                             // columns of O, D and the state a warp takes
+    extern __shared__ __align__(1024) unsigned char smem[];
+    unsigned char *sS = smem + M::S, *sI = smem + M::I;
+    float *tok = reinterpret_cast<float *>(smem + M::tok), *pw = reinterpret_cast<float *>(smem + M::pw);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + M::bars);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + M::slot);
+    volatile int *abort_flag = reinterpret_cast<int *>(smem + M::slot + 4);
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
+    const DecayArgs &A = P.a;
+
+    const int nseg = MAIN ? A.nseg : A.nseg - 1;
+    int id = blockIdx.x;
+    const int ip = id % A.npass; id /= A.npass;
+    const DecayPass &p = A.pass[ip];
+    const int seg = id % nseg, head = id / nseg, HX = MAIN ? p.HX : A.Hkv;
+    if (head >= A.B * HX) return;
+
+    if (tid == 0) {
+        for (int i = 0; i < TMA_BARS; ++i) mbar_init(bars + i, 1);
+        for (int i = TMA_BARS; i < NBARS; ++i) mbar_init(bars + i, kEpiWarps);
+        *abort_flag = (smem_u32(smem) & 1023u) ? 1 : 0;
+        fence_mbar_init();
+    }
+    if (warp == kEpiWarps) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
+    if (tid < 128) reinterpret_cast<uint32_t *>(sI)[tid] = 0;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (tid < 16) *reinterpret_cast<__nv_bfloat16 *>(sI + tid / 8 * (256 + 128) + tid % 8 * (16 + 2)) = __float2bfloat16_rn(1.f);
+    fence_async_smem();
+    pdl_wait_tma();
+    const uint32_t tmem = uniform(*tmem_slot);
+
+    const int b = head / HX, hx = head % HX, hs = hx / (HX / A.Hkv);
+    const int G = p.HY > HX ? p.HY / HX : 1;              // heads of Y that are summed over
+    const int hy0 = b * p.HY + (p.HY > HX ? hx * G : hx / (HX / p.HY));
+    const DecaySpan sp = decay_span<C>(A, b, seg);
+    const int a = p.a, c = p.c, nchunk = sp.k1 - sp.k0, items = nchunk * G;
+    const bool last_seg = sp.T == 0 ? seg == 0 : nchunk > 0 && sp.k1 == sp.T;
+    const size_t state = (size_t)(b * A.Hkv + hs) * a * c;
+    const float *S_in = nullptr;
+    float *S_out = nullptr;
+    if (MAIN) {
+        S_in = seg == 0 ? (p.S_in ? p.S_in + state : nullptr) : p.seg + ((size_t)(b * A.Hkv + hs) * (nseg - 1) + seg - 1) * a * c;
+        if (p.S_out && last_seg && hx % (HX / A.Hkv) == 0) S_out = p.S_out + state;
+    } else if (nchunk) S_out = const_cast<float *>(p.seg) + ((size_t)(b * A.Hkv + hs) * nseg + seg) * a * c;
+    const bool has0 = MAIN && S_in != nullptr;
+    if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
+    __syncthreads();
+
+    const auto first_row = [&](int k) { return (p.reverse ? sp.T - 1 - (sp.k0 + k) : sp.k0 + k) * C; };
+    int *status = A.status;
+
+    if (*abort_flag) {
+        if (tid == 0) atomicExch(status, (int)DARKATTN_ERR_CUDA);
+    } else if (warp == kEpiWarps) {                       // ------------------------------------------------ loads and stores
+        const TcMaps &m = P.m[ip];
+        bool ok = true;
+        for (int it = 0; it < items + 2 && ok; ++it) {
+            unsigned char *stage = smem + (it & 1) * M::kStage;
+            if (it >= 2) {                                // the stage's tiles have been used, and stored where rows out were staged in them
+                const int k = (it - 2) / G;
+                if (MAIN && (it - 2) % G == G - 1) {
+                    ok = warp_wait(bars + STAGED, k & 1, status, abort_flag);
+                    if (ok && sp.n - first_row(k) >= C && elect_one()) {
+                        for (int x = 0; x < DZ && x < c; x += 64) store3(&m.o, stage + x * 256, x, first_row(k), head);
+                        tma_store_commit();
+                        tma_store_wait_read();
+                    }
+                } else ok = warp_wait(bars + (MAIN ? PZ : DS), it & 1, status, abort_flag);
+                if (!ok) break;
+            }
+            if (it < items && elect_one()) {
+                const int t0 = first_row(it / G), hy = hy0 + it % G;
+                uint64_t *full = bars + FULL0 + (it & 1);
+                mbar_expect_tx(full, M::kStage);
+                if (MAIN) for (int x = 0; x < DY; x += 64) load3(stage + x * 256, &m.x, full, x, t0, head);
+                for (int x = 0; x < DY; x += 64) load3(stage + M::kX + x * 256, &m.y, full, x, t0, hy);
+                for (int x = 0; x < DZ; x += 64) load3(stage + M::kX + M::kY + x * 256, &m.z, full, x, t0, hy);
+            }
+        }
+        if (MAIN && elect_one()) tma_store_wait_all();
+    } else if (warp == kEpiWarps + 1) {                   // ------------------------------------------------ products
+        const uint32_t id_scores = make_idesc(128, 128, 0, 0), id_yt = make_idesc(128, 16, 1, 0), id_z = make_idesc(128, DZ, 0, 1);
+        const uint64_t eye = plain_desc(smem_u32(sI), 128, 256);
+        const TileDesc tS(sS);
+        bool ok = true;
+        int clean = 0;
+        for (int it = 0; it < items && ok; ++it) {
+            const unsigned char *stage = smem + (it & 1) * M::kStage;
+            const TileDesc tX(stage), tY(stage + M::kX), tZ(stage + M::kX + M::kY);
+            const int k = it / G, g = it % G;
+            ok = warp_wait(bars + FULL0 + (it & 1), (it >> 1) & 1, status, abort_flag);
+            if (ok && sp.n - first_row(k) < C) ok = warp_wait(bars + CLEAN, clean++ & 1, status, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                if (MAIN) {
+                    for (int q = 0; q < DY / 16; ++q) mma_ss(tmem + kA, kdesc(tX, q), kdesc(tY, q), id_scores, q > 0);
+                    mma_commit(bars + SCORES);
+                }
+                for (int q = 0; q < 8; ++q) mma_ss(tmem + kB + 16 * q, mndesc(tY, q), eye, id_yt, 0);
+                mma_commit(bars + YT);
+            }
+            const bool inter = has0 || k > 0;
+            if (g == 0) {
+                ok = warp_wait(bars + S_READY, k & 1, status, abort_flag);
+                if (MAIN && ok && k > 0) ok = warp_wait(bars + O_READ, (k - 1) & 1, status, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                if (MAIN && inter && elect_one()) {
+                    for (int q = 0; q < DY / 16; ++q) mma_ss(tmem + kO, kdesc(tX, q), mndesc(tS, q), id_z, q > 0);
+                    mma_commit(bars + INTER);
+                }
+            }
+            ok = warp_wait(bars + T_READY, it & 1, status, abort_flag);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                for (int part = 0; part < 3; ++part)
+                    for (int q = 0; q < 8; ++q)
+                        mma_ts(tmem + kD, tmem + (part < 2 ? kB + 64 * part : kA + 64) + 8 * q, mndesc(tZ, q), id_z, g > 0 || part > 0 || q > 0);
+                mma_commit(bars + DS);
+            }
+            if (MAIN) {
+                ok = warp_wait(bars + P_READY, it & 1, status, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    for (int q = 0; q < 8; ++q) mma_ts(tmem + kO, tmem + kA + 8 * q, mndesc(tZ, q), id_z, inter || g > 0 || q > 0);
+                    mma_commit(bars + PZ);
+                }
+            }
+        }
+    } else {                                              // ------------------------------------------------ 16 warps: what lies between
+        const int quarter = warp & 3, cb = warp >> 2, row = quarter * 32 + lane, z0 = cb * W;
+        const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
+        const bool rows_y = quarter * 32 < DY;            // this warp's lanes are rows of the state
+        __nv_bfloat16 *O = MAIN ? static_cast<__nv_bfloat16 *>(p.O) + (size_t)head * A.N * c : nullptr;
+        float s[W];                                       // the state: row `row`, columns z0 ..
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const int z = z0 + j;
+            s[j] = S_in && row < a && z < c ? (p.trans ? S_in[(size_t)z * a + row] : S_in[(size_t)row * c + z]) : 0.f;
+        }
+        const auto put_state = [&]() {                    // its copy for the product with the next chunk's rows
+            if (rows_y) {
+#pragma unroll
+                for (int q = 0; q < W / 8; ++q)
+                    *reinterpret_cast<uint4 *>(tile_chunk(sS, row, z0 / 8 + q)) =
+                        make_uint4(pack_bf16(s[8 * q], s[8 * q + 1]), pack_bf16(s[8 * q + 2], s[8 * q + 3]), pack_bf16(s[8 * q + 4], s[8 * q + 5]), pack_bf16(s[8 * q + 6], s[8 * q + 7]));
+                fence_async_smem();
+            }
+        };
+        if (has0) put_state();
+        mbar_arrive_warp(bars + S_READY);
+        // A wait that gave up ends all further waiting, not the loop: the warps still meet at their barriers, on numbers that mean nothing.
+        bool ok = true;
+#define DWAIT(bar, ph) do { if (ok) ok = warp_wait(bars + (bar), (ph), status, abort_flag); } while (0)
+        int Ltok = -1, inters = 0;
+        for (int it = 0; it < items; ++it) {
+            const int k = it / G, g = it % G, t0 = first_row(k), L = min(C, sp.n - t0);
+            if (L != Ltok) {                              // weights of a chunk's tokens: they change at a short chunk
+                epi_sync();
+                if (tid < C) tok[tid] = tid < L ? pw[p.reverse ? tid + 1 : L - 1 - tid] * p.tok_mul : 0.f;
+                epi_sync();
+                Ltok = L;
+            }
+            if (L < C) {                                  // rows behind the end are padding: zero, whatever they hold
+                DWAIT(FULL0 + (it & 1), (it >> 1) & 1);
+                unsigned char *y = smem + (it & 1) * M::kStage + M::kX;
+                const int per = (M::kY + M::kZ) / 16384 * 8;      // chunks of 16 bytes of a row of Y and Z
+                for (int i = tid; i < (C - L) * per; i += kEpiThreads) *reinterpret_cast<uint4 *>(tile_chunk(y, L + i / per, i % per)) = make_uint4(0, 0, 0, 0);
+                fence_async_smem();
+                mbar_arrive_warp(bars + CLEAN);
+            }
+            uint32_t v[32], pk[16];
+            if (MAIN) {                                   // P: the lower (backwards: the upper) triangle, times the decays
+                DWAIT(SCORES, it & 1);
+                tc_fence_after();
+                const bool off = p.reverse ? cb > quarter : cb < quarter;
+                if (off || cb == quarter) { tmem_ld32(at + kA + cb * 32, v); tmem_wait_ld(); }
+                quarter_sync(quarter);                    // P takes the place of scores that other warps read
+                if (off) {                                // lambda^|i - j| as a power for the row and one for the column, the block's near edge between
+                    const float r = p.p_mul * pw[p.reverse ? cb * 32 - row : row - cb * 32 - 31];
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        float x = f(v[j]) * r, y = f(v[j + 1]) * r;
+                        x *= pw[p.reverse ? j : 31 - j];
+                        y *= pw[p.reverse ? j + 1 : 30 - j];
+                        pk[j / 2] = pack_bf16(x, y);
+                    }
+                } else if (cb == quarter) {
+#pragma unroll
+                    for (int j = 0; j < 32; j += 2) {
+                        const int n0 = p.reverse ? j - lane : lane - j, n1 = p.reverse ? n0 + 1 : n0 - 1;
+                        const float x = n0 >= 0 ? f(v[j]) * (pw[n0] * p.p_mul) : 0.f, y = n1 >= 0 ? f(v[j + 1]) * (pw[n1] * p.p_mul) : 0.f;
+                        pk[j / 2] = pack_bf16(x, y);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) pk[j] = 0;
+                }
+                tmem_st16(at + kA + cb * 16, pk);
+            }
+            DWAIT(YT, it & 1);                            // tokens as columns: 32 of them
+            tc_fence_after();
+            if (rows_y) {
+                tmem_ld32(at + kB + cb * 32, v);
+                tmem_wait_ld();
+            }
+            quarter_sync(quarter);
+            if (rows_y) {
+                uint32_t p1[16], p2[16];
+#pragma unroll
+                for (int j = 0; j < 32; j += 2) split3(f(v[j]) * tok[cb * 32 + j], f(v[j + 1]) * tok[cb * 32 + j + 1], pk[j / 2], p1[j / 2], p2[j / 2]);
+                tmem_st16(at + kB + cb * 16, pk);
+                tmem_st16(at + kB + 64 + cb * 16, p1);
+                tmem_st16(at + kA + 64 + cb * 16, p2);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive_warp(bars + T_READY);
+            uint32_t o[W];
+            if (MAIN) {
+                if (g == 0 && (has0 || k > 0)) {
+                    DWAIT(INTER, inters & 1);
+                    ++inters;
+                    tc_fence_after();
+                    tmem_ld(at + kO + z0, o);
+                    tmem_wait_ld();
+                    const float r = row < L ? p.row_mul * pw[p.reverse ? L - 1 - row : row + 1] : 0.f;
+#pragma unroll
+                    for (int j = 0; j < W; ++j) o[j] = __float_as_uint(f(o[j]) * r);
+                    tmem_st(at + kO + z0, o);
+                    tmem_wait_st();
+                }
+                tc_fence_before();
+                mbar_arrive_warp(bars + P_READY);
+            }
+            DWAIT(DS, it & 1);
+            if (g == G - 1) {
+                tc_fence_after();
+                tmem_ld(at + kD + z0, o);
+                tmem_wait_ld();
+                const float keep = pw[L];
+#pragma unroll
+                for (int j = 0; j < W; ++j) s[j] = fmaf(keep, s[j], f(o[j]));
+                if (MAIN) put_state();
+                tc_fence_before();
+                mbar_arrive_warp(bars + S_READY);
+            }
+            if (MAIN) {
+                DWAIT(PZ, it & 1);
+                if (g == G - 1) {
+                    tc_fence_after();
+                    tmem_ld(at + kO + z0, o);
+                    tmem_wait_ld();
+                    tc_fence_before();
+                    mbar_arrive_warp(bars + O_READ);
+                    if (L == C) {
+#pragma unroll
+                        for (int q = 0; q < W / 8; ++q) *reinterpret_cast<uint4 *>(tile_chunk(smem + (it & 1) * M::kStage, row, z0 / 8 + q)) = pack8(o + 8 * q);
+                        fence_async_smem();
+                    } else if (row < L) {
+#pragma unroll
+                        for (int q = 0; q < W / 8; ++q)
+                            if (z0 + 8 * q < c) *reinterpret_cast<uint4 *>(O + (size_t)(t0 + row) * c + z0 + 8 * q) = pack8(o + 8 * q);
+                    }
+                    mbar_arrive_warp(bars + STAGED);
+                }
+            }
+        }
+#undef DWAIT
+        if (S_out && row < a) {
+#pragma unroll
+            for (int j = 0; j < W; j += 4)
+                if (z0 + j < c) *reinterpret_cast<float4 *>(S_out + (size_t)row * c + z0 + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+        }
+    }
+    __syncwarp();
+    if (*abort_flag) __nanosleep(200000);                 // copies that are still on their way
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kEpiWarps) tmem_dealloc(tmem, 512);
+}
+
+bool make_map3(CUtensorMap *m, const void *base, int heads, int N, int width)
+{
+    EncodeTiledFn enc = encode_fn();
+    if (!enc) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)width, (cuuint64_t)N, (cuuint64_t)heads}, strides[2] = {(cuuint64_t)width * 2, (cuuint64_t)width * 2 * (cuuint64_t)N};
+    const cuuint32_t box[3] = {64, C, 1}, es[3] = {1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DY, int DZ, bool MAIN>
+cudaError_t launch(const TcArgs &P, cudaStream_t st)
+{
+    int heads = 0;
+    for (int i = 0; i < P.a.npass; ++i) heads = max(heads, P.a.B * (MAIN ? P.a.pass[i].HX : P.a.Hkv));
+    const long long blocks = (long long)P.a.npass * heads * (MAIN ? P.a.nseg : P.a.nseg - 1);
+    return launch_pdl(decay_tc_kernel<DY, DZ, MAIN>, dim3((unsigned)blocks), dim3(kBlock), TcSmem<DY, DZ, MAIN>::total, st, P);
+}
+
+// passes whose widths are of one class share a launch
+template <bool MAIN>
+darkattn_status_t launch_all(const DecayArgs &A, const DecayPass *pass, int npass, cudaStream_t st)
+{
+    bool done[kDecayPasses] = {};
+    for (int i = 0; i < npass; ++i) {
+        if (done[i]) continue;
+        const bool y2 = pass[i].a > 64, z2 = pass[i].c > 64;
+        TcArgs P;
+        P.a = A;
+        int n = 0;
+        for (int j = i; j < npass; ++j) {
+            const DecayPass &q = pass[j];
+            if (done[j] || (q.a > 64) != y2 || (q.c > 64) != z2) continue;
+            done[j] = true;
+            P.a.pass[n] = q;
+            bool ok = make_map3(&P.m[n].y, q.Y, A.B * q.HY, A.N, q.a) && make_map3(&P.m[n].z, q.Z, A.B * q.HY, A.N, q.c);
+            if (MAIN) ok = ok && make_map3(&P.m[n].x, q.X, A.B * q.HX, A.N, q.a) && make_map3(&P.m[n].o, q.O, A.B * q.HX, A.N, q.c);
+            else P.m[n].x = P.m[n].o = P.m[n].y;
+            if (!ok) { set_cuda_error(cudaErrorInvalidValue, "decay: tensor map"); return DARKATTN_ERR_CUDA; }
+            ++n;
+        }
+        P.a.npass = n;
+        const cudaError_t e = y2 ? (z2 ? launch<128, 128, MAIN>(P, st) : launch<128, 64, MAIN>(P, st)) : (z2 ? launch<64, 128, MAIN>(P, st) : launch<64, 64, MAIN>(P, st));
+        DARKATTN_CUDA_TRY(e, "decay_tc_kernel");
+    }
+    return DARKATTN_OK;
+}
+
+}  // namespace
+
+bool decay_tc_supported(const darkattn_decay_desc_t &ds)
+{
+    return ds.dtype == DARKATTN_BF16 && ds.d % 8 == 0 && ds.dv % 8 == 0 && ds.d <= 128 && ds.dv <= 128;
+}
+
+// As for the FP32 kernels; in units of a chunk's time, one block an SM.
+static void pick(int T, long long units, long long state_units, int &nseg, int &cps)
+{
+    double best = 1e30;
+    for (int n = 1; n <= T && n <= 128; ++n) {
+        const int per = (T + n - 1) / n, m = (T + per - 1) / per;
+        double cost = (double)((units * m + 147) / 148) * (per + 1.5);
+        if (m > 1) cost += (double)((state_units * (m - 1) + 147) / 148) * (0.6 * per + 1.5) + 2 + 0.1 * m;
+        if (cost < best) { best = cost; nseg = m; cps = per; }
+    }
+}
+
+void decay_tc_split(darkattn_decay_plan_s *plan)
+{
+    const darkattn_decay_desc_t &ds = plan->desc;
+    const int T = (ds.N + C - 1) / C;
+    pick(T, (long long)ds.B * ds.H, (long long)ds.B * ds.H_kv, plan->fwd.nseg, plan->fwd.cps);
+    pick(T, 3LL * ds.B * ds.H, 2LL * ds.B * ds.H, plan->bwd.nseg, plan->bwd.cps);
+}
+
+darkattn_status_t decay_tc_run(DecayArgs &A, DecayPass *state_pass, int nstate, cudaStream_t st)
+{
+    DARKATTN_CUDA_TRY(cudaMemsetAsync(A.status, 0, sizeof(int), st), "decay: status");
+    if (A.nseg > 1) {
+        if (darkattn_status_t rc = launch_all<false>(A, state_pass, nstate, st)) return rc;
+        for (int i = 0; i < nstate; ++i) DARKATTN_CUDA_TRY(decay_scan_segments(A, state_pass[i], C, st), "decay_scan_kernel");
+    }
+    return launch_all<true>(A, A.pass, A.npass, st);
+}
+
+}  // namespace darkattn
