@@ -29,6 +29,7 @@ struct DecayPass {
     int reverse;                // direction
     int trans;                  // S is [c, a] in memory
     float p_mul, row_mul, tok_mul;   // tok_mul: of a token's share of the state
+    int whole;                  // (states of segments) the state reaches the caller
 };
 
 constexpr int kDecayPasses = 3;

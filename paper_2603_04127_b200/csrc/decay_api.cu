@@ -107,7 +107,7 @@ darkattn_status_t darkattn_decay_forward(darkattn_decay_plan_t plan, const void 
     DecayArgs A = common_args(plan, log_decay, lengths, plan->fwd.nseg, plan->fwd.cps, workspace);
     float *seg = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->ws.seg[0]);
     A.npass = 1;
-    A.pass[0] = DecayPass{Q, K, V, O, S_in, S_out, seg, ds.d, ds.dv, ds.H, ds.H_kv, 0, 0, ds.scale, ds.scale, 1.f};
+    A.pass[0] = DecayPass{Q, K, V, O, S_in, S_out, seg, ds.d, ds.dv, ds.H, ds.H_kv, 0, 0, ds.scale, ds.scale, 1.f, S_out != nullptr};
     DecayPass states = A.pass[0];
     return run(plan, A, &states, 1, st);
 }
@@ -126,10 +126,10 @@ darkattn_status_t darkattn_decay_backward(darkattn_decay_plan_t plan, const void
     DecayArgs A = common_args(plan, log_decay, lengths, plan->bwd.nseg, plan->bwd.cps, workspace);
     float *S = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->ws.seg[0]), *R = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->ws.seg[1]);
     A.npass = 3;
-    A.pass[0] = DecayPass{dO, V, K, dQ, S_in, nullptr, S, ds.dv, ds.d, ds.H, ds.H_kv, 0, 1, ds.scale, ds.scale, 1.f};
-    A.pass[1] = DecayPass{V, dO, Q, dK, dS_out, nullptr, R, ds.dv, ds.d, ds.H_kv, ds.H, 1, 1, ds.scale, 1.f, ds.scale};
-    A.pass[2] = DecayPass{K, Q, dO, dV, dS_out, dS_in, R, ds.d, ds.dv, ds.H_kv, ds.H, 1, 0, ds.scale, 1.f, ds.scale};
-    DecayPass sets[2] = {{nullptr, K, V, nullptr, S_in, nullptr, S, ds.d, ds.dv, ds.H_kv, ds.H_kv, 0, 0, 0.f, 0.f, 1.f}, A.pass[2]};
+    A.pass[0] = DecayPass{dO, V, K, dQ, S_in, nullptr, S, ds.dv, ds.d, ds.H, ds.H_kv, 0, 1, ds.scale, ds.scale, 1.f, 0};
+    A.pass[1] = DecayPass{V, dO, Q, dK, dS_out, nullptr, R, ds.dv, ds.d, ds.H_kv, ds.H, 1, 1, ds.scale, 1.f, ds.scale, 0};
+    A.pass[2] = DecayPass{K, Q, dO, dV, dS_out, dS_in, R, ds.d, ds.dv, ds.H_kv, ds.H, 1, 0, ds.scale, 1.f, ds.scale, dS_in != nullptr};
+    DecayPass sets[2] = {{nullptr, K, V, nullptr, S_in, nullptr, S, ds.d, ds.dv, ds.H_kv, ds.H_kv, 0, 0, 0.f, 0.f, 1.f, 0}, A.pass[2]};
     if (lengths) {
         const int e = ds.dtype == DARKATTN_BF16 ? 2 : 4;
         DARKATTN_CUDA_TRY(launch_pdl(decay_zero_tail_kernel, dim3((unsigned)(ds.H < 64 ? ds.H : 64), (unsigned)ds.B, 3), dim3(256), 0, st, static_cast<unsigned char *>(dQ), static_cast<unsigned char *>(dK),

@@ -1,11 +1,11 @@
 // Attention with a decay per head on the tensor cores: bf16 rows, chunks of 128, products with fp32 accumulation.
 //
-// One block takes a segment of one head's chunks in the pass's order; a chunk is five products of tcgen05.mma:
-//   A  = X Y^T                       scores; times the decays and rounded to bf16 they go back to tensor memory as P, the left operand of
-//   O  = lambda^(..) (X S) + P Z     the rows out: X S first, its rows scaled in place, P Z accumulated onto it
-//   Bt = Y^T I                       (16 tokens at a time) Y transposed into tensor memory (exact), where each token is a column: its weight is applied there in
-//                                    fp32, and the result goes back as three bf16 parts (together 24 bits), the left operands of
-//   D  = (w Y)^T Z                   what the chunk adds to the state
+// One block takes a segment of one head's chunks in the pass's order; a chunk is four products of tcgen05.mma:
+//   A = X Y^T                        scores; times the decays and rounded to bf16 they go back to tensor memory as P, the left operand of
+//   O = lambda^(..) (X S) + P Z      the rows out: X S first, its rows scaled in place, P Z accumulated onto it
+//   D = (w Y)^T Z                    what the chunk adds to the state. The tokens' weights are applied in fp32 to Y as it goes, transposed,
+//                                    from shared memory into tensor memory, as two bf16 parts (16 bits and their signs), or three (24)
+//                                    where the caller gets the state: with one, the rounding would show in the rows out.
 // The state itself stays in the registers of 16 warps in fp32, S <- lambda^L S + D; the rows read a copy rounded to bf16 (as P is
 // rounded: half a step of each term, like the rounding of the rows out).
 // Everything moves by TMA, two chunks of X, Y and Z deep; the rows out are staged in the chunk's own tiles.
@@ -22,13 +22,13 @@ constexpr uint32_t kA = 0, kB = 128, kO = 256, kD = 384; // columns of tensor me
 struct TcMaps { CUtensorMap x, y, z, o; };
 struct TcArgs { DecayArgs a; TcMaps m[kDecayPasses]; };
 
-enum { FULL0, FULL1, SCORES, YT, INTER, DS, PZ, TMA_BARS, P_READY = TMA_BARS, T_READY, S_READY, O_READ, STAGED, CLEAN, NBARS };
+enum { FULL0, FULL1, SCORES, INTER, DS, PZ, TMA_BARS, P_READY = TMA_BARS, T_READY, S_READY, O_READ, STAGED, CLEAN, NBARS };
 
 template <int DY, int DZ, bool MAIN>
 struct TcSmem {
     static constexpr int kX = MAIN ? DY / 64 * 16384 : 0, kY = DY / 64 * 16384, kZ = DZ / 64 * 16384;
     static constexpr int kStage = kX + kY + kZ;
-    static constexpr int S = 2 * kStage, I = S + (MAIN ? kZ : 0), tok = I + 512, pw = tok + 512, bars = pw + 528, slot = bars + NBARS * 8, total = slot + 16;
+    static constexpr int S = 2 * kStage, tok = S + (MAIN ? kZ : 0), near = tok + 512, pw = near + 128, bars = pw + 528, slot = bars + NBARS * 8, total = slot + 16;
     static_assert(total <= 232448, "shared memory of a block");
 };
 
@@ -43,8 +43,6 @@ __device__ __forceinline__ void store3(const CUtensorMap *map, const void *src, 
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z) : "memory");
 }
-// Matrix descriptor of an operand that is not swizzled: blocks of 8 rows of 16 bytes, lbo and sbo bytes apart.
-__device__ __forceinline__ uint64_t plain_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) { return make_sdesc(addr, lbo, sbo) & ~((uint64_t)7 << 61); }
 template <int N> __device__ __forceinline__ void tmem_ld(uint32_t a, uint32_t (&v)[N])
 {
     if constexpr (N == 32) tmem_ld32(a, v);
@@ -57,14 +55,23 @@ template <int N> __device__ __forceinline__ void tmem_st(uint32_t a, const uint3
 }
 __device__ __forceinline__ float f(uint32_t x) { return __uint_as_float(x); }
 
-// Two fp32 numbers as three pairs of bf16 parts; what is left of each is below 2^-25 of it.
-__device__ __forceinline__ void split3(float a, float b, uint32_t &p0, uint32_t &p1, uint32_t &p2)
+// Two fp32 numbers as pairs of bf16 parts: returns the leading ones, leaves what remains (exact) in a and b.
+__device__ __forceinline__ uint32_t take_part(float &a, float &b)
 {
-    p0 = pack_bf16(a, b);
-    a -= f(p0 << 16); b -= f(p0 & 0xffff0000u);
-    p1 = pack_bf16(a, b);
-    a -= f(p1 << 16); b -= f(p1 & 0xffff0000u);
-    p2 = pack_bf16(a, b);
+    const uint32_t p = pack_bf16(a, b);
+    add2(a, b, -f(p << 16), -f(p & 0xffff0000u));
+    return p;
+}
+// Four 8 x 8 matrices of 16-bit numbers, transposed: lane t receives of each the numbers 2 (t % 4) and the next of column t / 4.
+__device__ __forceinline__ void ldsm_t(uint32_t addr, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+// 16 lanes x 16 columns of tensor memory; lane t of the warp holds, of every four columns, column t % 4 of rows t / 4 and t / 4 + 8.
+__device__ __forceinline__ void tmem_st_16x128b(uint32_t a, const uint32_t (&v)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
 // MAIN: rows out; otherwise only the state of each of the first nseg - 1 segments, from zero, into pass.seg
@@ -74,8 +81,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     using M = TcSmem<DY, DZ, MAIN>;
     constexpr int W = DZ / 4;                             // columns of O, D and the state a warp takes
     extern __shared__ __align__(1024) unsigned char smem[];
-    unsigned char *sS = smem + M::S, *sI = smem + M::I;
-    float *tok = reinterpret_cast<float *>(smem + M::tok), *pw = reinterpret_cast<float *>(smem + M::pw);
+    unsigned char *sS = smem + M::S;
+    float *tok = reinterpret_cast<float *>(smem + M::tok), *near = reinterpret_cast<float *>(smem + M::near), *pw = reinterpret_cast<float *>(smem + M::pw);
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + M::bars);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + M::slot);
     volatile int *abort_flag = reinterpret_cast<int *>(smem + M::slot + 4);
@@ -96,12 +103,9 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         fence_mbar_init();
     }
     if (warp == kEpiWarps) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
-    if (tid < 128) reinterpret_cast<uint32_t *>(sI)[tid] = 0;
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (tid < 16) *reinterpret_cast<__nv_bfloat16 *>(sI + tid / 8 * (256 + 128) + tid % 8 * (16 + 2)) = __float2bfloat16_rn(1.f);
-    fence_async_smem();
     pdl_wait_tma();
     const uint32_t tmem = uniform(*tmem_slot);
 
@@ -119,8 +123,10 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         if (p.S_out && last_seg && hx % (HX / A.Hkv) == 0) S_out = p.S_out + state;
     } else if (nchunk) S_out = const_cast<float *>(p.seg) + ((size_t)(b * A.Hkv + hs) * nseg + seg) * a * c;
     const bool has0 = MAIN && S_in != nullptr;
+    const bool whole = MAIN ? S_out != nullptr : p.whole;   // three parts
     if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
     __syncthreads();
+    if (tid < 32) near[tid] = pw[p.reverse ? tid : 31 - tid];
 
     const auto first_row = [&](int k) { return (p.reverse ? sp.T - 1 - (sp.k0 + k) : sp.k0 + k) * C; };
     int *status = A.status;
@@ -155,45 +161,50 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         }
         if (MAIN && elect_one()) tma_store_wait_all();
     } else if (warp == kEpiWarps + 1) {                   // ------------------------------------------------ products
-        const uint32_t id_scores = make_idesc(128, 128, 0, 0), id_yt = make_idesc(128, 16, 1, 0), id_z = make_idesc(128, DZ, 0, 1);
-        const uint64_t eye = plain_desc(smem_u32(sI), 128, 256);
+        // In this order the pipe has something to do while the warps turn scores into P (X S, D), scale X S (D) and take the state (P Z).
+        const uint32_t id_scores = make_idesc(128, 128, 0, 0), id_z = make_idesc(128, DZ, 0, 1);
         const TileDesc tS(sS);
+        const int parts = whole ? 3 : 2;
         bool ok = true;
         int clean = 0;
         for (int it = 0; it < items && ok; ++it) {
             const unsigned char *stage = smem + (it & 1) * M::kStage;
             const TileDesc tX(stage), tY(stage + M::kX), tZ(stage + M::kX + M::kY);
             const int k = it / G, g = it % G;
-            ok = warp_wait(bars + FULL0 + (it & 1), (it >> 1) & 1, status, abort_flag);
-            if (ok && sp.n - first_row(k) < C) ok = warp_wait(bars + CLEAN, clean++ & 1, status, abort_flag);
-            if (!ok) break;
-            tc_fence_after();
-            if (elect_one()) {
-                if (MAIN) {
+            const bool inter = has0 || k > 0;
+            if (MAIN) {
+                ok = warp_wait(bars + FULL0 + (it & 1), (it >> 1) & 1, status, abort_flag);
+                if (ok && sp.n - first_row(k) < C) ok = warp_wait(bars + CLEAN, clean++ & 1, status, abort_flag);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+#pragma unroll
                     for (int q = 0; q < DY / 16; ++q) mma_ss(tmem + kA, kdesc(tX, q), kdesc(tY, q), id_scores, q > 0);
                     mma_commit(bars + SCORES);
                 }
-                for (int q = 0; q < 8; ++q) mma_ss(tmem + kB + 16 * q, mndesc(tY, q), eye, id_yt, 0);
-                mma_commit(bars + YT);
             }
-            const bool inter = has0 || k > 0;
             if (g == 0) {
                 ok = warp_wait(bars + S_READY, k & 1, status, abort_flag);
                 if (MAIN && ok && k > 0) ok = warp_wait(bars + O_READ, (k - 1) & 1, status, abort_flag);
                 if (!ok) break;
-                tc_fence_after();
-                if (MAIN && inter && elect_one()) {
-                    for (int q = 0; q < DY / 16; ++q) mma_ss(tmem + kO, kdesc(tX, q), mndesc(tS, q), id_z, q > 0);
-                    mma_commit(bars + INTER);
+                if (MAIN && inter) {
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int q = 0; q < DY / 16; ++q) mma_ss(tmem + kO, kdesc(tX, q), mndesc(tS, q), id_z, q > 0);
+                        mma_commit(bars + INTER);
+                    }
                 }
             }
             ok = warp_wait(bars + T_READY, it & 1, status, abort_flag);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-                for (int part = 0; part < 3; ++part)
-                    for (int q = 0; q < 8; ++q)
-                        mma_ts(tmem + kD, tmem + (part < 2 ? kB + 64 * part : kA + 64) + 8 * q, mndesc(tZ, q), id_z, g > 0 || part > 0 || q > 0);
+                for (int part = 0; part < parts; ++part) {
+                    const uint32_t left = tmem + (part < 2 ? kB + 64 * part : kA + 64);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) mma_ts(tmem + kD, left + 8 * q, mndesc(tZ, q), id_z, g > 0 || part > 0 || q > 0);
+                }
                 mma_commit(bars + DS);
             }
             if (MAIN) {
@@ -201,6 +212,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
+#pragma unroll
                     for (int q = 0; q < 8; ++q) mma_ts(tmem + kO, tmem + kA + 8 * q, mndesc(tZ, q), id_z, inter || g > 0 || q > 0);
                     mma_commit(bars + PZ);
                 }
@@ -231,90 +243,130 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         // A wait that gave up ends all further waiting, not the loop: the warps still meet at their barriers, on numbers that mean nothing.
         bool ok = true;
 #define DWAIT(bar, ph) do { if (ok) ok = warp_wait(bars + (bar), (ph), status, abort_flag); } while (0)
+        // This warp's 32 columns and 32 tokens of w Y, from shared memory (tokens are rows) to tensor memory (tokens are columns): the first
+        // two parts, or the third.
+        const auto transpose = [&](int it, bool third) {
+            const uint32_t tile = smem_u32(smem + (it & 1) * M::kStage + M::kX);
+            const int t = cb * 32 + ((lane >> 4) & 1) * 8 + (lane & 7), ch = quarter * 4 + ((lane >> 3) & 1);      // of the matrix row this lane points at
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t p0[8], p1[8];
+#pragma unroll
+                for (int tg = 0; tg < 2; ++tg) {
+                    uint32_t r[4];
+                    ldsm_t(tile + ((ch + 2 * h) >> 3) * 16384 + swz128(t + 16 * tg, (ch + 2 * h) & 7), r);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        const float2 w = *reinterpret_cast<const float2 *>(tok + cb * 32 + tg * 16 + (m >> 1) * 8 + 2 * (lane & 3));
+                        float x = f(r[m] << 16), y = f(r[m] & 0xffff0000u);
+                        mul2(x, y, w.x, w.y);
+                        p0[tg * 4 + m] = take_part(x, y);
+                        if (third) take_part(x, y);
+                        p1[tg * 4 + m] = pack_bf16(x, y);
+                    }
+                }
+                const uint32_t to = at + ((uint32_t)(16 * h) << 16) + cb * 16;
+                if (!third) tmem_st_16x128b(to + kB, p0);
+                tmem_st_16x128b(to + (third ? kA + 64 : kB + 64), p1);
+            }
+        };
         int Ltok = -1, inters = 0;
-        for (int it = 0; it < items; ++it) {
-            const int k = it / G, g = it % G, t0 = first_row(k), L = min(C, sp.n - t0);
-            if (L != Ltok) {                              // weights of a chunk's tokens: they change at a short chunk
-                epi_sync();
+        // Brings item `it`'s weighted Y into tensor memory (what of the third part's place there is free only behind the scores).
+        const auto prepare = [&](int it) {
+            const int L = min(C, sp.n - first_row(it / G));
+            DWAIT(FULL0 + (it & 1), (it >> 1) & 1);
+            if (L != Ltok || L < C) {
+                epi_sync();                               // the weights of the chunk before have been used
                 if (tid < C) tok[tid] = tid < L ? pw[p.reverse ? tid + 1 : L - 1 - tid] * p.tok_mul : 0.f;
+                if (L < C) {                              // rows behind the end are padding: zero, whatever they hold
+                    unsigned char *y = smem + (it & 1) * M::kStage + M::kX;
+                    const int per = (M::kY + M::kZ) / 16384 * 8;      // chunks of 16 bytes of a row of Y and Z
+                    for (int i = tid; i < (C - L) * per; i += kEpiThreads) *reinterpret_cast<uint4 *>(tile_chunk(y, L + i / per, i % per)) = make_uint4(0, 0, 0, 0);
+                    fence_async_smem();
+                }
                 epi_sync();
+                if (L < C) mbar_arrive_warp(bars + CLEAN);
                 Ltok = L;
             }
-            if (L < C) {                                  // rows behind the end are padding: zero, whatever they hold
-                DWAIT(FULL0 + (it & 1), (it >> 1) & 1);
-                unsigned char *y = smem + (it & 1) * M::kStage + M::kX;
-                const int per = (M::kY + M::kZ) / 16384 * 8;      // chunks of 16 bytes of a row of Y and Z
-                for (int i = tid; i < (C - L) * per; i += kEpiThreads) *reinterpret_cast<uint4 *>(tile_chunk(y, L + i / per, i % per)) = make_uint4(0, 0, 0, 0);
-                fence_async_smem();
-                mbar_arrive_warp(bars + CLEAN);
-            }
-            uint32_t v[32], pk[16];
+            if (rows_y) transpose(it, false);
+            if (MAIN && whole) return;
+            if (!MAIN && whole && rows_y) transpose(it, true);
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive_warp(bars + T_READY);
+        };
+        if (items > 0) prepare(0);
+        for (int it = 0; it < items; ++it) {
+            const int k = it / G, g = it % G, t0 = first_row(k), L = min(C, sp.n - t0);
             if (MAIN) {                                   // P: the lower (backwards: the upper) triangle, times the decays
                 DWAIT(SCORES, it & 1);
                 tc_fence_after();
                 const bool off = p.reverse ? cb > quarter : cb < quarter;
-                if (off || cb == quarter) { tmem_ld32(at + kA + cb * 32, v); tmem_wait_ld(); }
-                quarter_sync(quarter);                    // P takes the place of scores that other warps read
+                uint32_t pk[16];
                 if (off) {                                // lambda^|i - j| as a power for the row and one for the column, the block's near edge between
                     const float r = p.p_mul * pw[p.reverse ? cb * 32 - row : row - cb * 32 - 31];
 #pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        float x = f(v[j]) * r, y = f(v[j + 1]) * r;
-                        x *= pw[p.reverse ? j : 31 - j];
-                        y *= pw[p.reverse ? j + 1 : 30 - j];
-                        pk[j / 2] = pack_bf16(x, y);
+                    for (int h = 0; h < 32; h += 16) {
+                        uint32_t v[16];
+                        tmem_ld16(at + kA + cb * 32 + h, v);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 16; j += 4) {
+                            const float4 w = *reinterpret_cast<const float4 *>(near + h + j);
+                            float x[4] = {f(v[j]), f(v[j + 1]), f(v[j + 2]), f(v[j + 3])};
+                            mul2(x[0], x[1], r, r);
+                            mul2(x[2], x[3], r, r);
+                            mul2(x[0], x[1], w.x, w.y);
+                            mul2(x[2], x[3], w.z, w.w);
+                            pk[(h + j) / 2] = pack_bf16(x[0], x[1]);
+                            pk[(h + j) / 2 + 1] = pack_bf16(x[2], x[3]);
+                        }
                     }
                 } else if (cb == quarter) {
 #pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        const int n0 = p.reverse ? j - lane : lane - j, n1 = p.reverse ? n0 + 1 : n0 - 1;
-                        const float x = n0 >= 0 ? f(v[j]) * (pw[n0] * p.p_mul) : 0.f, y = n1 >= 0 ? f(v[j + 1]) * (pw[n1] * p.p_mul) : 0.f;
-                        pk[j / 2] = pack_bf16(x, y);
+                    for (int h = 0; h < 32; h += 16) {
+                        uint32_t v[16];
+                        tmem_ld16(at + kA + cb * 32 + h, v);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 16; j += 2) {
+                            const int n0 = p.reverse ? h + j - lane : lane - h - j, n1 = p.reverse ? n0 + 1 : n0 - 1;
+                            const float w0 = pw[max(n0, 0)] * p.p_mul, w1 = pw[max(n1, 0)] * p.p_mul;
+                            pk[(h + j) / 2] = pack_bf16(n0 >= 0 ? f(v[j]) * w0 : 0.f, n1 >= 0 ? f(v[j + 1]) * w1 : 0.f);
+                        }
                     }
                 } else {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) pk[j] = 0;
                 }
+                quarter_sync(quarter);                    // P takes the place of scores that other warps read
                 tmem_st16(at + kA + cb * 16, pk);
-            }
-            DWAIT(YT, it & 1);                            // tokens as columns: 32 of them
-            tc_fence_after();
-            if (rows_y) {
-                tmem_ld32(at + kB + cb * 32, v);
-                tmem_wait_ld();
-            }
-            quarter_sync(quarter);
-            if (rows_y) {
-                uint32_t p1[16], p2[16];
-#pragma unroll
-                for (int j = 0; j < 32; j += 2) split3(f(v[j]) * tok[cb * 32 + j], f(v[j + 1]) * tok[cb * 32 + j + 1], pk[j / 2], p1[j / 2], p2[j / 2]);
-                tmem_st16(at + kB + cb * 16, pk);
-                tmem_st16(at + kB + 64 + cb * 16, p1);
-                tmem_st16(at + kA + 64 + cb * 16, p2);
-            }
-            tmem_wait_st();
-            tc_fence_before();
-            mbar_arrive_warp(bars + T_READY);
-            uint32_t o[W];
-            if (MAIN) {
+                if (whole) {
+                    if (rows_y) transpose(it, true);
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive_warp(bars + T_READY);
+                }
                 if (g == 0 && (has0 || k > 0)) {
                     DWAIT(INTER, inters & 1);
                     ++inters;
                     tc_fence_after();
+                    uint32_t o[W];
                     tmem_ld(at + kO + z0, o);
                     tmem_wait_ld();
                     const float r = row < L ? p.row_mul * pw[p.reverse ? L - 1 - row : row + 1] : 0.f;
 #pragma unroll
                     for (int j = 0; j < W; ++j) o[j] = __float_as_uint(f(o[j]) * r);
                     tmem_st(at + kO + z0, o);
-                    tmem_wait_st();
                 }
+                tmem_wait_st();
                 tc_fence_before();
                 mbar_arrive_warp(bars + P_READY);
             }
             DWAIT(DS, it & 1);
             if (g == G - 1) {
                 tc_fence_after();
+                uint32_t o[W];
                 tmem_ld(at + kD + z0, o);
                 tmem_wait_ld();
                 const float keep = pw[L];
@@ -328,6 +380,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 DWAIT(PZ, it & 1);
                 if (g == G - 1) {
                     tc_fence_after();
+                    uint32_t o[W];
                     tmem_ld(at + kO + z0, o);
                     tmem_wait_ld();
                     tc_fence_before();
@@ -344,6 +397,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     mbar_arrive_warp(bars + STAGED);
                 }
             }
+            if (it + 1 < items) prepare(it + 1);
         }
 #undef DWAIT
         if (S_out && row < a) {
