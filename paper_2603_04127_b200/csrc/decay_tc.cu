@@ -18,6 +18,9 @@ using namespace tc;
 
 constexpr int C = 128, kBlock = 576;                     // 16 warps, one that loads and stores, one that issues products
 constexpr uint32_t kA = 0, kB = 128, kO = 256, kD = 384; // columns of tensor memory
+constexpr uint32_t kX = 320;                             // X S of a narrow Z (64 columns), apart from P Z; of a wide one it goes to kO
+constexpr uint32_t kThirdWide = kA + 64, kThirdNarrow = 448;      // the third part of w Y: the half of the scores' columns that P does not take, or columns of its own
+constexpr int kDiag = 68;                                // numbers of each copy of the diagonal blocks' decays
 
 struct TcMaps { CUtensorMap x, y, z, o; };
 struct TcArgs { DecayArgs a; TcMaps m[kDecayPasses]; };
@@ -28,7 +31,7 @@ template <int DY, int DZ, bool MAIN>
 struct TcSmem {
     static constexpr int kX = MAIN ? DY / 64 * 16384 : 0, kY = DY / 64 * 16384, kZ = DZ / 64 * 16384;
     static constexpr int kStage = kX + kY + kZ;
-    static constexpr int S = 2 * kStage, tok = S + (MAIN ? kZ : 0), near = tok + 512, pw = near + 128, bars = pw + 528, slot = bars + NBARS * 8, total = slot + 16;
+    static constexpr int S = 2 * kStage, tok = S + (MAIN ? kZ : 0), near = tok + 512, diag = near + 128, pw = diag + 4 * kDiag * 4, bars = pw + 528, slot = bars + NBARS * 8, total = slot + 16;
     static_assert(total <= 232448, "shared memory of a block");
 };
 
@@ -55,11 +58,27 @@ template <int N> __device__ __forceinline__ void tmem_st(uint32_t a, const uint3
 }
 __device__ __forceinline__ float f(uint32_t x) { return __uint_as_float(x); }
 
+// Waits with a limit on the number of tries: the timer and the flag of tc::warp_wait cost a block of 64-column tiles a tenth of its time. A try
+// that finds nothing suspends the warp for a while, so that a healthy wait takes a few of them. One answer for the warp.
+constexpr int kTries = 1 << 22;
+__device__ __forceinline__ bool wait_tries(uint64_t *bar, uint32_t parity, int *status, volatile int *abort_flag)
+{
+    bool ok = false;
+#pragma unroll 1
+    for (int i = 0; i < kTries; ++i) {
+        ok = mbar_try_wait(bar, parity);
+        if (ok) break;
+        if ((i & 4095) == 4095 && *abort_flag) break;
+    }
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok) { *abort_flag = 1; atomicExch(status, 5 /* DARKATTN_ERR_TIMEOUT */); }
+    return ok;
+}
 // Two fp32 numbers as pairs of bf16 parts: returns the leading ones, leaves what remains (exact) in a and b.
 __device__ __forceinline__ uint32_t take_part(float &a, float &b)
 {
     const uint32_t p = pack_bf16(a, b);
-    add2(a, b, -f(p << 16), -f(p & 0xffff0000u));
+    fma2(a, b, f(p << 16), f(p & 0xffff0000u), -1.f, -1.f);
     return p;
 }
 // Four 8 x 8 matrices of 16-bit numbers, transposed: lane t receives of each the numbers 2 (t % 4) and the next of column t / 4.
@@ -82,7 +101,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     constexpr int W = DZ / 4;                             // columns of O, D and the state a warp takes
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char *sS = smem + M::S;
-    float *tok = reinterpret_cast<float *>(smem + M::tok), *near = reinterpret_cast<float *>(smem + M::near), *pw = reinterpret_cast<float *>(smem + M::pw);
+    float *tok = reinterpret_cast<float *>(smem + M::tok), *near = reinterpret_cast<float *>(smem + M::near), *diag = reinterpret_cast<float *>(smem + M::diag), *pw = reinterpret_cast<float *>(smem + M::pw);
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + M::bars);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + M::slot);
     volatile int *abort_flag = reinterpret_cast<int *>(smem + M::slot + 4);
@@ -126,7 +145,13 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     const bool whole = MAIN ? S_out != nullptr : p.whole;   // three parts
     if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
     __syncthreads();
-    if (tid < 32) near[tid] = pw[p.reverse ? tid : 31 - tid];
+    // Decays of a block of 32 x 32 scores by column, times p_mul: from the near edge where the block is off the diagonal; on it, where row r needs
+    // lambda^|r - j| (0 behind it), four copies, each shifted by one, let every row read its 32 numbers four at a time: copy r % 4 from 32 - r / 4 * 4 on.
+    if (tid < 32) near[tid] = p.p_mul * pw[p.reverse ? tid : 31 - tid];
+    if (tid < 4 * kDiag) {
+        const int j = tid % kDiag - 32 - tid / kDiag, n = p.reverse ? j : -j;       // column less row
+        diag[tid] = n >= 0 && n < 32 ? p.p_mul * pw[n] : 0.f;
+    }
 
     const auto first_row = [&](int k) { return (p.reverse ? sp.T - 1 - (sp.k0 + k) : sp.k0 + k) * C; };
     int *status = A.status;
@@ -141,13 +166,13 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             if (it >= 2) {                                // the stage's tiles have been used, and stored where rows out were staged in them
                 const int k = (it - 2) / G;
                 if (MAIN && (it - 2) % G == G - 1) {
-                    ok = warp_wait(bars + STAGED, k & 1, status, abort_flag);
+                    ok = wait_tries(bars + STAGED, k & 1, status, abort_flag);
                     if (ok && sp.n - first_row(k) >= C && elect_one()) {
                         for (int x = 0; x < DZ && x < c; x += 64) store3(&m.o, stage + x * 256, x, first_row(k), head);
                         tma_store_commit();
                         tma_store_wait_read();
                     }
-                } else ok = warp_wait(bars + (MAIN ? PZ : DS), it & 1, status, abort_flag);
+                } else ok = wait_tries(bars + (MAIN ? PZ : DS), it & 1, status, abort_flag);
                 if (!ok) break;
             }
             if (it < items && elect_one()) {
@@ -173,8 +198,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             const int k = it / G, g = it % G;
             const bool inter = has0 || k > 0;
             if (MAIN) {
-                ok = warp_wait(bars + FULL0 + (it & 1), (it >> 1) & 1, status, abort_flag);
-                if (ok && sp.n - first_row(k) < C) ok = warp_wait(bars + CLEAN, clean++ & 1, status, abort_flag);
+                ok = wait_tries(bars + FULL0 + (it & 1), (it >> 1) & 1, status, abort_flag);
+                if (ok && sp.n - first_row(k) < C) ok = wait_tries(bars + CLEAN, clean++ & 1, status, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
@@ -184,36 +209,36 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 }
             }
             if (g == 0) {
-                ok = warp_wait(bars + S_READY, k & 1, status, abort_flag);
-                if (MAIN && ok && k > 0) ok = warp_wait(bars + O_READ, (k - 1) & 1, status, abort_flag);
+                ok = wait_tries(bars + S_READY, k & 1, status, abort_flag);
+                if (MAIN && ok && k > 0) ok = wait_tries(bars + O_READ, (k - 1) & 1, status, abort_flag);
                 if (!ok) break;
                 if (MAIN && inter) {
                     tc_fence_after();
                     if (elect_one()) {
 #pragma unroll
-                        for (int q = 0; q < DY / 16; ++q) mma_ss(tmem + kO, kdesc(tX, q), mndesc(tS, q), id_z, q > 0);
+                        for (int q = 0; q < DY / 16; ++q) mma_ss(tmem + (DZ == 64 ? kX : kO), kdesc(tX, q), mndesc(tS, q), id_z, q > 0);
                         mma_commit(bars + INTER);
                     }
                 }
             }
-            ok = warp_wait(bars + T_READY, it & 1, status, abort_flag);
+            ok = wait_tries(bars + T_READY, it & 1, status, abort_flag);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
                 for (int part = 0; part < parts; ++part) {
-                    const uint32_t left = tmem + (part < 2 ? kB + 64 * part : kA + 64);
+                    const uint32_t left = tmem + (part < 2 ? kB + 64 * part : DZ == 64 ? kThirdNarrow : kThirdWide);
 #pragma unroll
                     for (int q = 0; q < 8; ++q) mma_ts(tmem + kD, left + 8 * q, mndesc(tZ, q), id_z, g > 0 || part > 0 || q > 0);
                 }
                 mma_commit(bars + DS);
             }
             if (MAIN) {
-                ok = warp_wait(bars + P_READY, it & 1, status, abort_flag);
+                ok = wait_tries(bars + P_READY, it & 1, status, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) mma_ts(tmem + kO, tmem + kA + 8 * q, mndesc(tZ, q), id_z, inter || g > 0 || q > 0);
+                    for (int q = 0; q < 8; ++q) mma_ts(tmem + kO, tmem + kA + 8 * q, mndesc(tZ, q), id_z, (DZ == 128 && inter) || g > 0 || q > 0);
                     mma_commit(bars + PZ);
                 }
             }
@@ -242,36 +267,39 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         mbar_arrive_warp(bars + S_READY);
         // A wait that gave up ends all further waiting, not the loop: the warps still meet at their barriers, on numbers that mean nothing.
         bool ok = true;
-#define DWAIT(bar, ph) do { if (ok) ok = warp_wait(bars + (bar), (ph), status, abort_flag); } while (0)
+#define DWAIT(bar, ph) do { if (ok) ok = wait_tries(bars + (bar), (ph), status, abort_flag); } while (0)
         // This warp's 32 columns and 32 tokens of w Y, from shared memory (tokens are rows) to tensor memory (tokens are columns): the first
         // two parts, or the third.
         const auto transpose = [&](int it, bool third) {
             const uint32_t tile = smem_u32(smem + (it & 1) * M::kStage + M::kX);
             const int t = cb * 32 + ((lane >> 4) & 1) * 8 + (lane & 7), ch = quarter * 4 + ((lane >> 3) & 1);      // of the matrix row this lane points at
+            uint32_t y[2][2][4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int tg = 0; tg < 2; ++tg) ldsm_t(tile + ((ch + 2 * h) >> 3) * 16384 + swz128(t + 16 * tg, (ch + 2 * h) & 7), y[h][tg]);
+            float2 w[4];                                  // of tokens 2 (lane % 4) and the next of every eight
+#pragma unroll
+            for (int m = 0; m < 4; ++m) w[m] = *reinterpret_cast<const float2 *>(tok + cb * 32 + m * 8 + 2 * (lane & 3));
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t p0[8], p1[8];
 #pragma unroll
-                for (int tg = 0; tg < 2; ++tg) {
-                    uint32_t r[4];
-                    ldsm_t(tile + ((ch + 2 * h) >> 3) * 16384 + swz128(t + 16 * tg, (ch + 2 * h) & 7), r);
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        const float2 w = *reinterpret_cast<const float2 *>(tok + cb * 32 + tg * 16 + (m >> 1) * 8 + 2 * (lane & 3));
-                        float x = f(r[m] << 16), y = f(r[m] & 0xffff0000u);
-                        mul2(x, y, w.x, w.y);
-                        p0[tg * 4 + m] = take_part(x, y);
-                        if (third) take_part(x, y);
-                        p1[tg * 4 + m] = pack_bf16(x, y);
-                    }
+                for (int m = 0; m < 8; ++m) {
+                    const uint32_t r = y[h][m >> 2][m & 3];
+                    float u = f(r << 16), v = f(r & 0xffff0000u);
+                    mul2(u, v, w[m >> 1].x, w[m >> 1].y);
+                    p0[m] = take_part(u, v);
+                    if (third) take_part(u, v);
+                    p1[m] = pack_bf16(u, v);
                 }
                 const uint32_t to = at + ((uint32_t)(16 * h) << 16) + cb * 16;
                 if (!third) tmem_st_16x128b(to + kB, p0);
-                tmem_st_16x128b(to + (third ? kA + 64 : kB + 64), p1);
+                tmem_st_16x128b(to + (!third ? kB + 64 : DZ == 64 ? kThirdNarrow : kThirdWide), p1);
             }
         };
         int Ltok = -1, inters = 0;
-        // Brings item `it`'s weighted Y into tensor memory (what of the third part's place there is free only behind the scores).
+        // Brings item `it`'s weighted Y into tensor memory.
         const auto prepare = [&](int it) {
             const int L = min(C, sp.n - first_row(it / G));
             DWAIT(FULL0 + (it & 1), (it >> 1) & 1);
@@ -289,8 +317,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 Ltok = L;
             }
             if (rows_y) transpose(it, false);
-            if (MAIN && whole) return;
-            if (!MAIN && whole && rows_y) transpose(it, true);
+            if (MAIN && DZ == 128 && whole) return;         // the third part follows when the scores have been read
+            if (whole && rows_y) transpose(it, true);
             tmem_wait_st();
             tc_fence_before();
             mbar_arrive_warp(bars + T_READY);
@@ -303,16 +331,19 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 tc_fence_after();
                 const bool off = p.reverse ? cb > quarter : cb < quarter;
                 uint32_t pk[16];
-                if (off) {                                // lambda^|i - j| as a power for the row and one for the column, the block's near edge between
-                    const float r = p.p_mul * pw[p.reverse ? cb * 32 - row : row - cb * 32 - 31];
+                if (off || cb == quarter) {               // by column, and off the diagonal a power for the row, up to the block's near edge
+                    const float r = off ? pw[p.reverse ? cb * 32 - row : row - cb * 32 - 31] : 1.f;
+                    const float *by = off ? near : diag + (lane & 3) * kDiag + 32 - (lane & ~3);
+                    constexpr int kLd = DZ == 64 ? 32 : 16;      // (registers)
 #pragma unroll
-                    for (int h = 0; h < 32; h += 16) {
-                        uint32_t v[16];
-                        tmem_ld16(at + kA + cb * 32 + h, v);
+                    for (int h = 0; h < 32; h += kLd) {
+                        uint32_t v[kLd];
+                        if constexpr (kLd == 32) tmem_ld32(at + kA + cb * 32, v);
+                        else tmem_ld16(at + kA + cb * 32 + h, v);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int j = 0; j < 16; j += 4) {
-                            const float4 w = *reinterpret_cast<const float4 *>(near + h + j);
+                        for (int j = 0; j < kLd; j += 4) {
+                            const float4 w = *reinterpret_cast<const float4 *>(by + h + j);
                             float x[4] = {f(v[j]), f(v[j + 1]), f(v[j + 2]), f(v[j + 3])};
                             mul2(x[0], x[1], r, r);
                             mul2(x[2], x[3], r, r);
@@ -322,32 +353,19 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                             pk[(h + j) / 2 + 1] = pack_bf16(x[2], x[3]);
                         }
                     }
-                } else if (cb == quarter) {
-#pragma unroll
-                    for (int h = 0; h < 32; h += 16) {
-                        uint32_t v[16];
-                        tmem_ld16(at + kA + cb * 32 + h, v);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int j = 0; j < 16; j += 2) {
-                            const int n0 = p.reverse ? h + j - lane : lane - h - j, n1 = p.reverse ? n0 + 1 : n0 - 1;
-                            const float w0 = pw[max(n0, 0)] * p.p_mul, w1 = pw[max(n1, 0)] * p.p_mul;
-                            pk[(h + j) / 2] = pack_bf16(n0 >= 0 ? f(v[j]) * w0 : 0.f, n1 >= 0 ? f(v[j + 1]) * w1 : 0.f);
-                        }
-                    }
                 } else {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) pk[j] = 0;
                 }
                 quarter_sync(quarter);                    // P takes the place of scores that other warps read
                 tmem_st16(at + kA + cb * 16, pk);
-                if (whole) {
+                if (DZ == 128 && whole) {
                     if (rows_y) transpose(it, true);
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive_warp(bars + T_READY);
                 }
-                if (g == 0 && (has0 || k > 0)) {
+                if (DZ == 128 && g == 0 && (has0 || k > 0)) {
                     DWAIT(INTER, inters & 1);
                     ++inters;
                     tc_fence_after();
@@ -382,6 +400,14 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     tc_fence_after();
                     uint32_t o[W];
                     tmem_ld(at + kO + z0, o);
+                    if (DZ == 64 && (has0 || k > 0)) {
+                        uint32_t x[W];
+                        tmem_ld(at + kX + z0, x);
+                        tmem_wait_ld();
+                        const float r = row < L ? p.row_mul * pw[p.reverse ? L - 1 - row : row + 1] : 0.f;
+#pragma unroll
+                        for (int j = 0; j < W; ++j) o[j] = __float_as_uint(fmaf(f(x[j]), r, f(o[j])));
+                    }
                     tmem_wait_ld();
                     tc_fence_before();
                     mbar_arrive_warp(bars + O_READ);
