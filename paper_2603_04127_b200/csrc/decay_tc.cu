@@ -82,9 +82,9 @@ __device__ __forceinline__ uint32_t take_part(float &a, float &b)
     return p;
 }
 // Four 8 x 8 matrices of 16-bit numbers, transposed: lane t receives of each the numbers 2 (t % 4) and the next of column t / 4.
-__device__ __forceinline__ void ldsm_t(uint32_t addr, uint32_t (&r)[4])
+__device__ __forceinline__ void ldsm_t(uint32_t addr, uint32_t &r0, uint32_t &r1, uint32_t &r2, uint32_t &r3)
 {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr) : "memory");
 }
 // 16 lanes x 16 columns of tensor memory; lane t of the warp holds, of every four columns, column t % 4 of rows t / 4 and t / 4 + 8.
 __device__ __forceinline__ void tmem_st_16x128b(uint32_t a, const uint32_t (&v)[8])
@@ -93,12 +93,45 @@ __device__ __forceinline__ void tmem_st_16x128b(uint32_t a, const uint32_t (&v)[
                  ::"r"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
+// 32 columns of Y (numbers 32 quarter ..) and 32 of its tokens (32 cb ..), times their weights, from shared memory (tokens are rows) to tensor
+// memory (tokens are columns, two to a column): the first two parts, 64 columns apart, or the third.
+template <bool THIRD>
+__device__ __forceinline__ void weighted_transpose(uint32_t tile, const float *weights, uint32_t to, int quarter, int cb, int lane)
+{
+    const int t = cb * 32 + ((lane >> 4) & 1) * 8 + (lane & 7), ch = quarter * 4 + ((lane >> 3) & 1);      // of the matrix row this lane points at
+    uint32_t y[2][8];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int tg = 0; tg < 2; ++tg)
+            ldsm_t(tile + ((ch + 2 * h) >> 3) * 16384 + swz128(t + 16 * tg, (ch + 2 * h) & 7), y[h][4 * tg], y[h][4 * tg + 1], y[h][4 * tg + 2], y[h][4 * tg + 3]);
+    float2 w[4];                                          // of tokens 2 (lane % 4) and the next of every eight
+#pragma unroll
+    for (int m = 0; m < 4; ++m) w[m] = *reinterpret_cast<const float2 *>(weights + m * 8 + 2 * (lane & 3));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t p0[8], p1[8];
+#pragma unroll
+        for (int m = 0; m < 8; ++m) {
+            float u = f(y[h][m] << 16), v = f(y[h][m] & 0xffff0000u);
+            mul2(u, v, w[m >> 1].x, w[m >> 1].y);
+            p0[m] = take_part(u, v);
+            if (THIRD) take_part(u, v);
+            p1[m] = pack_bf16(u, v);
+        }
+        const uint32_t at = to + ((uint32_t)(16 * h) << 16);
+        if (!THIRD) tmem_st_16x128b(at, p0);
+        tmem_st_16x128b(at + (THIRD ? 0 : 64), p1);
+    }
+}
+
 // MAIN: rows out; otherwise only the state of each of the first nseg - 1 segments, from zero, into pass.seg
 template <int DY, int DZ, bool MAIN>
 __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_constant__ TcArgs P)
 {
     using M = TcSmem<DY, DZ, MAIN>;
     constexpr int W = DZ / 4;                             // columns of O, D and the state a warp takes
+    constexpr uint32_t kThird = DZ == 64 ? kThirdNarrow : kThirdWide;
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char *sS = smem + M::S;
     float *tok = reinterpret_cast<float *>(smem + M::tok), *near = reinterpret_cast<float *>(smem + M::near), *diag = reinterpret_cast<float *>(smem + M::diag), *pw = reinterpret_cast<float *>(smem + M::pw);
@@ -132,7 +165,10 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     const int G = p.HY > HX ? p.HY / HX : 1;              // heads of Y that are summed over
     const int hy0 = b * p.HY + (p.HY > HX ? hx * G : hx / (HX / p.HY));
     const DecaySpan sp = decay_span<C>(A, b, seg);
-    const int a = p.a, c = p.c, nchunk = sp.k1 - sp.k0, items = nchunk * G;
+    // (in registers for good: read where they are used, parameters miss the constant cache)
+    const int reverse = uniform(p.reverse), a = uniform(p.a), c = uniform(p.c);
+    const float row_mul = __int_as_float(uniform(__float_as_int(p.row_mul)));
+    const int nchunk = sp.k1 - sp.k0, items = nchunk * G;
     const bool last_seg = sp.T == 0 ? seg == 0 : nchunk > 0 && sp.k1 == sp.T;
     const size_t state = (size_t)(b * A.Hkv + hs) * a * c;
     const float *S_in = nullptr;
@@ -153,7 +189,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         diag[tid] = n >= 0 && n < 32 ? p.p_mul * pw[n] : 0.f;
     }
 
-    const auto first_row = [&](int k) { return (p.reverse ? sp.T - 1 - (sp.k0 + k) : sp.k0 + k) * C; };
+    const auto first_row = [&](int k) { return (reverse ? sp.T - 1 - (sp.k0 + k) : sp.k0 + k) * C; };
     int *status = A.status;
 
     if (*abort_flag) {
@@ -161,27 +197,30 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     } else if (warp == kEpiWarps) {                       // ------------------------------------------------ loads and stores
         const TcMaps &m = P.m[ip];
         bool ok = true;
-        for (int it = 0; it < items + 2 && ok; ++it) {
+        for (int it = 0, k = 0, g = 0, k2 = 0, g2 = 0; it < items + 2 && ok; ++it) {      // (k, g): chunk and head of item `it`, (k2, g2) of the one two before
             unsigned char *stage = smem + (it & 1) * M::kStage;
             if (it >= 2) {                                // the stage's tiles have been used, and stored where rows out were staged in them
-                const int k = (it - 2) / G;
-                if (MAIN && (it - 2) % G == G - 1) {
-                    ok = wait_tries(bars + STAGED, k & 1, status, abort_flag);
-                    if (ok && sp.n - first_row(k) >= C && elect_one()) {
-                        for (int x = 0; x < DZ && x < c; x += 64) store3(&m.o, stage + x * 256, x, first_row(k), head);
+                if (MAIN && g2 == G - 1) {
+                    ok = wait_tries(bars + STAGED, k2 & 1, status, abort_flag);
+                    if (ok && sp.n - first_row(k2) >= C && elect_one()) {
+                        for (int x = 0; x < DZ && x < c; x += 64) store3(&m.o, stage + x * 256, x, first_row(k2), head);
                         tma_store_commit();
                         tma_store_wait_read();
                     }
                 } else ok = wait_tries(bars + (MAIN ? PZ : DS), it & 1, status, abort_flag);
                 if (!ok) break;
+                if (++g2 == G) { g2 = 0; ++k2; }
             }
-            if (it < items && elect_one()) {
-                const int t0 = first_row(it / G), hy = hy0 + it % G;
-                uint64_t *full = bars + FULL0 + (it & 1);
-                mbar_expect_tx(full, M::kStage);
-                if (MAIN) for (int x = 0; x < DY; x += 64) load3(stage + x * 256, &m.x, full, x, t0, head);
-                for (int x = 0; x < DY; x += 64) load3(stage + M::kX + x * 256, &m.y, full, x, t0, hy);
-                for (int x = 0; x < DZ; x += 64) load3(stage + M::kX + M::kY + x * 256, &m.z, full, x, t0, hy);
+            if (it < items) {
+                if (elect_one()) {
+                    const int t0 = first_row(k), hy = hy0 + g;
+                    uint64_t *full = bars + FULL0 + (it & 1);
+                    mbar_expect_tx(full, M::kStage);
+                    if (MAIN) for (int x = 0; x < DY; x += 64) load3(stage + x * 256, &m.x, full, x, t0, head);
+                    for (int x = 0; x < DY; x += 64) load3(stage + M::kX + x * 256, &m.y, full, x, t0, hy);
+                    for (int x = 0; x < DZ; x += 64) load3(stage + M::kX + M::kY + x * 256, &m.z, full, x, t0, hy);
+                }
+                if (++g == G) { g = 0; ++k; }
             }
         }
         if (MAIN && elect_one()) tma_store_wait_all();
@@ -192,10 +231,9 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         const int parts = whole ? 3 : 2;
         bool ok = true;
         int clean = 0;
-        for (int it = 0; it < items && ok; ++it) {
+        for (int it = 0, k = 0, g = 0; it < items && ok; ++it, k += g + 1 == G, g = g + 1 == G ? 0 : g + 1) {
             const unsigned char *stage = smem + (it & 1) * M::kStage;
             const TileDesc tX(stage), tY(stage + M::kX), tZ(stage + M::kX + M::kY);
-            const int k = it / G, g = it % G;
             const bool inter = has0 || k > 0;
             if (MAIN) {
                 ok = wait_tries(bars + FULL0 + (it & 1), (it >> 1) & 1, status, abort_flag);
@@ -226,7 +264,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             tc_fence_after();
             if (elect_one()) {
                 for (int part = 0; part < parts; ++part) {
-                    const uint32_t left = tmem + (part < 2 ? kB + 64 * part : DZ == 64 ? kThirdNarrow : kThirdWide);
+                    const uint32_t left = tmem + (part < 2 ? kB + 64 * part : kThird);
 #pragma unroll
                     for (int q = 0; q < 8; ++q) mma_ts(tmem + kD, left + 8 * q, mndesc(tZ, q), id_z, g > 0 || part > 0 || q > 0);
                 }
@@ -268,44 +306,13 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         // A wait that gave up ends all further waiting, not the loop: the warps still meet at their barriers, on numbers that mean nothing.
         bool ok = true;
 #define DWAIT(bar, ph) do { if (ok) ok = wait_tries(bars + (bar), (ph), status, abort_flag); } while (0)
-        // This warp's 32 columns and 32 tokens of w Y, from shared memory (tokens are rows) to tensor memory (tokens are columns): the first
-        // two parts, or the third.
-        const auto transpose = [&](int it, bool third) {
-            const uint32_t tile = smem_u32(smem + (it & 1) * M::kStage + M::kX);
-            const int t = cb * 32 + ((lane >> 4) & 1) * 8 + (lane & 7), ch = quarter * 4 + ((lane >> 3) & 1);      // of the matrix row this lane points at
-            uint32_t y[2][2][4];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int tg = 0; tg < 2; ++tg) ldsm_t(tile + ((ch + 2 * h) >> 3) * 16384 + swz128(t + 16 * tg, (ch + 2 * h) & 7), y[h][tg]);
-            float2 w[4];                                  // of tokens 2 (lane % 4) and the next of every eight
-#pragma unroll
-            for (int m = 0; m < 4; ++m) w[m] = *reinterpret_cast<const float2 *>(tok + cb * 32 + m * 8 + 2 * (lane & 3));
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t p0[8], p1[8];
-#pragma unroll
-                for (int m = 0; m < 8; ++m) {
-                    const uint32_t r = y[h][m >> 2][m & 3];
-                    float u = f(r << 16), v = f(r & 0xffff0000u);
-                    mul2(u, v, w[m >> 1].x, w[m >> 1].y);
-                    p0[m] = take_part(u, v);
-                    if (third) take_part(u, v);
-                    p1[m] = pack_bf16(u, v);
-                }
-                const uint32_t to = at + ((uint32_t)(16 * h) << 16) + cb * 16;
-                if (!third) tmem_st_16x128b(to + kB, p0);
-                tmem_st_16x128b(to + (!third ? kB + 64 : DZ == 64 ? kThirdNarrow : kThirdWide), p1);
-            }
-        };
         int Ltok = -1, inters = 0;
-        // Brings item `it`'s weighted Y into tensor memory.
-        const auto prepare = [&](int it) {
-            const int L = min(C, sp.n - first_row(it / G));
+        // Brings item `it`'s weighted Y (of a chunk of L rows) into tensor memory.
+        const auto prepare = [&](int it, int L) {
             DWAIT(FULL0 + (it & 1), (it >> 1) & 1);
             if (L != Ltok || L < C) {
                 epi_sync();                               // the weights of the chunk before have been used
-                if (tid < C) tok[tid] = tid < L ? pw[p.reverse ? tid + 1 : L - 1 - tid] * p.tok_mul : 0.f;
+                if (tid < C) tok[tid] = tid < L ? pw[reverse ? tid + 1 : L - 1 - tid] * p.tok_mul : 0.f;
                 if (L < C) {                              // rows behind the end are padding: zero, whatever they hold
                     unsigned char *y = smem + (it & 1) * M::kStage + M::kX;
                     const int per = (M::kY + M::kZ) / 16384 * 8;      // chunks of 16 bytes of a row of Y and Z
@@ -316,24 +323,26 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 if (L < C) mbar_arrive_warp(bars + CLEAN);
                 Ltok = L;
             }
-            if (rows_y) transpose(it, false);
+            if (rows_y) weighted_transpose<false>(smem_u32(smem + (it & 1) * M::kStage + M::kX), tok + cb * 32, at + kB + cb * 16, quarter, cb, lane);
             if (MAIN && DZ == 128 && whole) return;         // the third part follows when the scores have been read
-            if (whole && rows_y) transpose(it, true);
+            if (whole && rows_y) weighted_transpose<true>(smem_u32(smem + (it & 1) * M::kStage + M::kX), tok + cb * 32, at + kThird + cb * 16, quarter, cb, lane);
             tmem_wait_st();
             tc_fence_before();
             mbar_arrive_warp(bars + T_READY);
         };
-        if (items > 0) prepare(0);
-        for (int it = 0; it < items; ++it) {
-            const int k = it / G, g = it % G, t0 = first_row(k), L = min(C, sp.n - t0);
+        const auto rows_of = [&](int k) { return min(C, sp.n - first_row(k)); };
+        // P of a block off the diagonal: by column, and a power for the row, up to the block's near edge; on the diagonal by a table alone.
+        const bool off = reverse ? cb > quarter : cb < quarter;
+        const float p_row = off ? pw[reverse ? cb * 32 - row : row - cb * 32 - 31] : 1.f;
+        const float *p_col = off ? near : diag + (lane & 3) * kDiag + 32 - (lane & ~3);
+        if (items > 0) prepare(0, rows_of(0));
+        for (int it = 0, k = 0, g = 0; it < items; ++it) {
+            const int t0 = first_row(k), L = min(C, sp.n - t0);
             if (MAIN) {                                   // P: the lower (backwards: the upper) triangle, times the decays
                 DWAIT(SCORES, it & 1);
                 tc_fence_after();
-                const bool off = p.reverse ? cb > quarter : cb < quarter;
                 uint32_t pk[16];
-                if (off || cb == quarter) {               // by column, and off the diagonal a power for the row, up to the block's near edge
-                    const float r = off ? pw[p.reverse ? cb * 32 - row : row - cb * 32 - 31] : 1.f;
-                    const float *by = off ? near : diag + (lane & 3) * kDiag + 32 - (lane & ~3);
+                if (off || cb == quarter) {
                     constexpr int kLd = DZ == 64 ? 32 : 16;      // (registers)
 #pragma unroll
                     for (int h = 0; h < 32; h += kLd) {
@@ -343,10 +352,10 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                         tmem_wait_ld();
 #pragma unroll
                         for (int j = 0; j < kLd; j += 4) {
-                            const float4 w = *reinterpret_cast<const float4 *>(by + h + j);
+                            const float4 w = *reinterpret_cast<const float4 *>(p_col + h + j);
                             float x[4] = {f(v[j]), f(v[j + 1]), f(v[j + 2]), f(v[j + 3])};
-                            mul2(x[0], x[1], r, r);
-                            mul2(x[2], x[3], r, r);
+                            mul2(x[0], x[1], p_row, p_row);
+                            mul2(x[2], x[3], p_row, p_row);
                             mul2(x[0], x[1], w.x, w.y);
                             mul2(x[2], x[3], w.z, w.w);
                             pk[(h + j) / 2] = pack_bf16(x[0], x[1]);
@@ -360,7 +369,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 quarter_sync(quarter);                    // P takes the place of scores that other warps read
                 tmem_st16(at + kA + cb * 16, pk);
                 if (DZ == 128 && whole) {
-                    if (rows_y) transpose(it, true);
+                    if (rows_y) weighted_transpose<true>(smem_u32(smem + (it & 1) * M::kStage + M::kX), tok + cb * 32, at + kThird + cb * 16, quarter, cb, lane);
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive_warp(bars + T_READY);
@@ -372,7 +381,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     uint32_t o[W];
                     tmem_ld(at + kO + z0, o);
                     tmem_wait_ld();
-                    const float r = row < L ? p.row_mul * pw[p.reverse ? L - 1 - row : row + 1] : 0.f;
+                    const float r = row < L ? row_mul * pw[reverse ? L - 1 - row : row + 1] : 0.f;
 #pragma unroll
                     for (int j = 0; j < W; ++j) o[j] = __float_as_uint(f(o[j]) * r);
                     tmem_st(at + kO + z0, o);
@@ -404,7 +413,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                         uint32_t x[W];
                         tmem_ld(at + kX + z0, x);
                         tmem_wait_ld();
-                        const float r = row < L ? p.row_mul * pw[p.reverse ? L - 1 - row : row + 1] : 0.f;
+                        const float r = row < L ? row_mul * pw[reverse ? L - 1 - row : row + 1] : 0.f;
 #pragma unroll
                         for (int j = 0; j < W; ++j) o[j] = __float_as_uint(fmaf(f(x[j]), r, f(o[j])));
                     }
@@ -423,7 +432,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     mbar_arrive_warp(bars + STAGED);
                 }
             }
-            if (it + 1 < items) prepare(it + 1);
+            if (++g == G) { g = 0; ++k; }
+            if (it + 1 < items) prepare(it + 1, rows_of(k));
         }
 #undef DWAIT
         if (S_out && row < a) {
