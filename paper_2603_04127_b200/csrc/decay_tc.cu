@@ -16,7 +16,14 @@ namespace darkattn {
 namespace {
 using namespace tc;
 
-constexpr int C = 128, kBlock = 576;                     // 16 warps, one that loads and stores, one that issues products
+constexpr int C = 128;
+// Column groups: kGroups warps share a quarter of the rows, each takes DZ / kGroups columns of O, D and the state. Beside them one warp
+// loads and stores, one issues products.
+#ifndef NCOLS
+#define NCOLS 4
+#endif
+constexpr int kGroups = NCOLS, kWarps = 4 * kGroups, kBlock = 32 * (kWarps + 2);
+static_assert(kGroups == 2 || kGroups == 4, "blocks of scores are shared out for these");
 constexpr uint32_t kA = 0, kB = 128, kO = 256, kD = 384; // columns of tensor memory
 constexpr uint32_t kX = 320;                             // X S of a narrow Z (64 columns), apart from P Z; of a wide one it goes to kO
 constexpr uint32_t kThirdWide = kA + 64, kThirdNarrow = 448;      // the third part of w Y: the half of the scores' columns that P does not take, or columns of its own
@@ -58,28 +65,51 @@ template <int N> __device__ __forceinline__ void tmem_st(uint32_t a, const uint3
 }
 __device__ __forceinline__ float f(uint32_t x) { return __uint_as_float(x); }
 
-// Waits with a limit on the number of tries: the timer and the flag of tc::warp_wait cost a block of 64-column tiles a tenth of its time. A try
-// that finds nothing suspends the warp for a while, so that a healthy wait takes a few of them. One answer for the warp.
-constexpr int kTries = 1 << 22;
-__device__ __forceinline__ bool wait_tries(uint64_t *bar, uint32_t parity, int *status, volatile int *abort_flag)
+// Shared memory by its 32-bit addresses: all of a block's are one number, read once, and constants.
+// A wait with a limit on the number of tries; one answer for the warp. The timer and the flag of tc::warp_wait cost a block of 64-column
+// tiles a tenth of its time. A try that finds nothing suspends the warp for a while, so that a healthy wait takes a few of them.
+__device__ __forceinline__ bool wait_tries(uint32_t bar, uint32_t parity, int *status)
 {
-    bool ok = false;
-#pragma unroll 1
-    for (int i = 0; i < kTries; ++i) {
-        ok = mbar_try_wait(bar, parity);
-        if (ok) break;
-        if ((i & 4095) == 4095 && *abort_flag) break;
-    }
-    ok = __all_sync(0xffffffffu, ok);
-    if (!ok) { *abort_flag = 1; atomicExch(status, 5 /* DARKATTN_ERR_TIMEOUT */); }
-    return ok;
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 2097152;\n\t"
+        "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
+        "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n\t"
+        "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    if (__all_sync(0xffffffffu, ok)) return true;
+    atomicExch(status, 5 /* DARKATTN_ERR_TIMEOUT */);
+    return false;
 }
+__device__ __forceinline__ void arrive_warp(uint32_t bar, int lane)
+{
+    __syncwarp();
+    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void sts16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+template <int N> __device__ __forceinline__ void quarter_bar(int q) { asm volatile("bar.sync %0, %1;" ::"r"(q + 1), "n"(N) : "memory"); }
+template <int N> __device__ __forceinline__ void warps_bar() { asm volatile("bar.sync 5, %0;" ::"n"(N) : "memory"); }
 // Two fp32 numbers as pairs of bf16 parts: returns the leading ones, leaves what remains (exact) in a and b.
 __device__ __forceinline__ uint32_t take_part(float &a, float &b)
 {
     const uint32_t p = pack_bf16(a, b);
     fma2(a, b, f(p << 16), f(p & 0xffff0000u), -1.f, -1.f);
     return p;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t c)
+{
+    uint32_t d;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
 }
 // Four 8 x 8 matrices of 16-bit numbers, transposed: lane t receives of each the numbers 2 (t % 4) and the next of column t / 4.
 __device__ __forceinline__ void ldsm_t(uint32_t addr, uint32_t &r0, uint32_t &r1, uint32_t &r2, uint32_t &r3)
@@ -93,35 +123,48 @@ __device__ __forceinline__ void tmem_st_16x128b(uint32_t a, const uint32_t (&v)[
                  ::"r"(a), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 
-// 32 columns of Y (numbers 32 quarter ..) and 32 of its tokens (32 cb ..), times their weights, from shared memory (tokens are rows) to tensor
-// memory (tokens are columns, two to a column): the first two parts, 64 columns apart, or the third.
-template <bool THIRD>
-__device__ __forceinline__ void weighted_transpose(uint32_t tile, const float *weights, uint32_t to, int quarter, int cb, int lane)
+// 32 columns of Y and 32 of its tokens, times their weights, from shared memory (tokens are rows) to tensor
+// memory (tokens are columns, two to a column).
+//   TWO        two parts, formed in packed bf16 arithmetic from the weights' own two parts w1 + w2: p = y w1, rounded; y w1 - p is exact in 8 bits;
+//              with y w2 added it is the second part. Off by 2^-16 of the number at most, and 3 instructions for two numbers where
+//              unpacking, a product in fp32 and taking it apart are 8 (the transposition of a chunk: 1100 cycles)
+//   LEAD       the first two of three parts, from an fp32 weight;  THIRD: the third;  ALL: three
+enum { TWO, LEAD, THIRD, ALL };
+template <int MODE>
+__device__ __forceinline__ void weighted_transpose(uint32_t from, const float *weights, uint32_t to, uint32_t to3)
 {
-    const int t = cb * 32 + ((lane >> 4) & 1) * 8 + (lane & 7), ch = quarter * 4 + ((lane >> 3) & 1);      // of the matrix row this lane points at
+    // from: the address of this lane's matrix row of the first 16 tokens and columns; 16 more columns are two 16-byte chunks (a swizzled bit) on
     uint32_t y[2][8];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int tg = 0; tg < 2; ++tg)
-            ldsm_t(tile + ((ch + 2 * h) >> 3) * 16384 + swz128(t + 16 * tg, (ch + 2 * h) & 7), y[h][4 * tg], y[h][4 * tg + 1], y[h][4 * tg + 2], y[h][4 * tg + 3]);
-    float2 w[4];                                          // of tokens 2 (lane % 4) and the next of every eight
+        for (int tg = 0; tg < 2; ++tg) ldsm_t((from ^ (h << 5)) + tg * 2048, y[h][4 * tg], y[h][4 * tg + 1], y[h][4 * tg + 2], y[h][4 * tg + 3]);
+    float2 w[4];                                          // of tokens 2 (lane % 4) and the next of every eight (TWO: pairs of first and of second parts)
 #pragma unroll
-    for (int m = 0; m < 4; ++m) w[m] = *reinterpret_cast<const float2 *>(weights + m * 8 + 2 * (lane & 3));
+    for (int m = 0; m < 4; ++m) w[m] = *reinterpret_cast<const float2 *>(weights + m * 8);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        uint32_t p0[8], p1[8];
+        const uint32_t lanes = (uint32_t)(16 * h) << 16;
+        uint32_t p0[8], p1[8], p2[8];
 #pragma unroll
         for (int m = 0; m < 8; ++m) {
-            float u = f(y[h][m] << 16), v = f(y[h][m] & 0xffff0000u);
-            mul2(u, v, w[m >> 1].x, w[m >> 1].y);
-            p0[m] = take_part(u, v);
-            if (THIRD) take_part(u, v);
-            p1[m] = pack_bf16(u, v);
+            if (MODE == TWO) {
+                const uint32_t w1 = __float_as_uint(w[m >> 1].x), w2 = __float_as_uint(w[m >> 1].y);
+                p0[m] = mul_bf16x2(y[h][m], w1);
+                p1[m] = fma_bf16x2(y[h][m], w2, fma_bf16x2(y[h][m], w1, p0[m] ^ 0x80008000u));
+            } else {
+                float u = f(y[h][m] << 16), v = f(y[h][m] & 0xffff0000u);
+                mul2(u, v, w[m >> 1].x, w[m >> 1].y);
+                p0[m] = take_part(u, v);
+                p1[m] = take_part(u, v);
+                p2[m] = pack_bf16(u, v);
+            }
         }
-        const uint32_t at = to + ((uint32_t)(16 * h) << 16);
-        if (!THIRD) tmem_st_16x128b(at, p0);
-        tmem_st_16x128b(at + (THIRD ? 0 : 64), p1);
+        if (MODE != THIRD) {
+            tmem_st_16x128b(to + lanes, p0);
+            tmem_st_16x128b(to + 64 + lanes, p1);
+        }
+        if (MODE >= THIRD) tmem_st_16x128b(to3 + lanes, p2);
     }
 }
 
@@ -130,15 +173,21 @@ template <int DY, int DZ, bool MAIN>
 __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_constant__ TcArgs P)
 {
     using M = TcSmem<DY, DZ, MAIN>;
-    constexpr int W = DZ / 4;                             // columns of O, D and the state a warp takes
+    constexpr int W = DZ / kGroups;                       // columns of O, D and the state a warp takes
     constexpr uint32_t kThird = DZ == 64 ? kThirdNarrow : kThirdWide;
+    constexpr bool kBehindScores = MAIN && DZ == 128;
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char *sS = smem + M::S;
     float *tok = reinterpret_cast<float *>(smem + M::tok), *near = reinterpret_cast<float *>(smem + M::near), *diag = reinterpret_cast<float *>(smem + M::diag), *pw = reinterpret_cast<float *>(smem + M::pw);
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + M::bars);
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(smem + M::slot);
     volatile int *abort_flag = reinterpret_cast<int *>(smem + M::slot + 4);
-    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
+    const int tid = threadIdx.x, warp = uniform(tid >> 5);
+    int lane;
+    asm volatile("mov.u32 %0, %%laneid;" : "=r"(lane));
+    uint32_t sbase;
+    asm volatile("mov.u32 %0, %1;" : "=r"(sbase) : "r"(smem_u32(smem)));
+    const uint32_t bar = sbase + M::bars;                 // 8 bytes each
     const DecayArgs &A = P.a;
 
     const int nseg = MAIN ? A.nseg : A.nseg - 1;
@@ -150,11 +199,11 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
 
     if (tid == 0) {
         for (int i = 0; i < TMA_BARS; ++i) mbar_init(bars + i, 1);
-        for (int i = TMA_BARS; i < NBARS; ++i) mbar_init(bars + i, kEpiWarps);
+        for (int i = TMA_BARS; i < NBARS; ++i) mbar_init(bars + i, kWarps);
         *abort_flag = (smem_u32(smem) & 1023u) ? 1 : 0;
         fence_mbar_init();
     }
-    if (warp == kEpiWarps) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
+    if (warp == kWarps) { tmem_alloc(tmem_slot, 512); tmem_relinquish(); }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -184,30 +233,31 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     // Decays of a block of 32 x 32 scores by column, times p_mul: from the near edge where the block is off the diagonal; on it, where row r needs
     // lambda^|r - j| (0 behind it), four copies, each shifted by one, let every row read its 32 numbers four at a time: copy r % 4 from 32 - r / 4 * 4 on.
     if (tid < 32) near[tid] = p.p_mul * pw[p.reverse ? tid : 31 - tid];
-    if (tid < 4 * kDiag) {
-        const int j = tid % kDiag - 32 - tid / kDiag, n = p.reverse ? j : -j;       // column less row
-        diag[tid] = n >= 0 && n < 32 ? p.p_mul * pw[n] : 0.f;
+    for (int i = tid; i < 4 * kDiag; i += kBlock) {
+        const int j = i % kDiag - 32 - i / kDiag, n = p.reverse ? j : -j;       // column less row
+        diag[i] = n >= 0 && n < 32 ? p.p_mul * pw[n] : 0.f;
     }
+    __syncthreads();
 
     const auto first_row = [&](int k) { return (reverse ? sp.T - 1 - (sp.k0 + k) : sp.k0 + k) * C; };
     int *status = A.status;
 
     if (*abort_flag) {
         if (tid == 0) atomicExch(status, (int)DARKATTN_ERR_CUDA);
-    } else if (warp == kEpiWarps) {                       // ------------------------------------------------ loads and stores
+    } else if (warp == kWarps) {                       // ------------------------------------------------ loads and stores
         const TcMaps &m = P.m[ip];
         bool ok = true;
         for (int it = 0, k = 0, g = 0, k2 = 0, g2 = 0; it < items + 2 && ok; ++it) {      // (k, g): chunk and head of item `it`, (k2, g2) of the one two before
             unsigned char *stage = smem + (it & 1) * M::kStage;
             if (it >= 2) {                                // the stage's tiles have been used, and stored where rows out were staged in them
                 if (MAIN && g2 == G - 1) {
-                    ok = wait_tries(bars + STAGED, k2 & 1, status, abort_flag);
+                    ok = wait_tries(bar + 8 * STAGED, k2 & 1, status);
                     if (ok && sp.n - first_row(k2) >= C && elect_one()) {
                         for (int x = 0; x < DZ && x < c; x += 64) store3(&m.o, stage + x * 256, x, first_row(k2), head);
                         tma_store_commit();
                         tma_store_wait_read();
                     }
-                } else ok = wait_tries(bars + (MAIN ? PZ : DS), it & 1, status, abort_flag);
+                } else ok = wait_tries(bar + 8 * (MAIN ? PZ : DS), it & 1, status);
                 if (!ok) break;
                 if (++g2 == G) { g2 = 0; ++k2; }
             }
@@ -224,7 +274,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             }
         }
         if (MAIN && elect_one()) tma_store_wait_all();
-    } else if (warp == kEpiWarps + 1) {                   // ------------------------------------------------ products
+        if (!ok) *abort_flag = 1;
+    } else if (warp == kWarps + 1) {                   // ------------------------------------------------ products
         // In this order the pipe has something to do while the warps turn scores into P (X S, D), scale X S (D) and take the state (P Z).
         const uint32_t id_scores = make_idesc(128, 128, 0, 0), id_z = make_idesc(128, DZ, 0, 1);
         const TileDesc tS(sS);
@@ -236,8 +287,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             const TileDesc tX(stage), tY(stage + M::kX), tZ(stage + M::kX + M::kY);
             const bool inter = has0 || k > 0;
             if (MAIN) {
-                ok = wait_tries(bars + FULL0 + (it & 1), (it >> 1) & 1, status, abort_flag);
-                if (ok && sp.n - first_row(k) < C) ok = wait_tries(bars + CLEAN, clean++ & 1, status, abort_flag);
+                ok = wait_tries(bar + 8 * (FULL0 + (it & 1)), (it >> 1) & 1, status);
+                if (ok && sp.n - first_row(k) < C) ok = wait_tries(bar + 8 * CLEAN, clean++ & 1, status);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
@@ -247,8 +298,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 }
             }
             if (g == 0) {
-                ok = wait_tries(bars + S_READY, k & 1, status, abort_flag);
-                if (MAIN && ok && k > 0) ok = wait_tries(bars + O_READ, (k - 1) & 1, status, abort_flag);
+                ok = wait_tries(bar + 8 * S_READY, k & 1, status);
+                if (MAIN && ok && k > 0) ok = wait_tries(bar + 8 * O_READ, (k - 1) & 1, status);
                 if (!ok) break;
                 if (MAIN && inter) {
                     tc_fence_after();
@@ -259,7 +310,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     }
                 }
             }
-            ok = wait_tries(bars + T_READY, it & 1, status, abort_flag);
+            ok = wait_tries(bar + 8 * T_READY, it & 1, status);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -271,7 +322,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 mma_commit(bars + DS);
             }
             if (MAIN) {
-                ok = wait_tries(bars + P_READY, it & 1, status, abort_flag);
+                ok = wait_tries(bar + 8 * P_READY, it & 1, status);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
@@ -281,10 +332,13 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 }
             }
         }
-    } else {                                              // ------------------------------------------------ 16 warps: what lies between
+        if (!ok) *abort_flag = 1;
+    } else {                                              // ------------------------------------------------ what lies between the products
         const int quarter = warp & 3, cb = warp >> 2, row = quarter * 32 + lane, z0 = cb * W;
         const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
         const bool rows_y = quarter * 32 < DY;            // this warp's lanes are rows of the state
+        const uint32_t own = (uint32_t)((z0 >> 6) * 16384 + row * 128 + ((((z0 >> 3) & 7) ^ (row & 7)) << 4));      // this lane's first 16 bytes in a swizzled tile
+        const uint32_t y_own = (uint32_t)(M::kX + (quarter >> 1) * 16384 + (((lane >> 4) & 1) * 8 + (lane & 7)) * 128 + ((((quarter & 1) * 4 + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
         __nv_bfloat16 *O = MAIN ? static_cast<__nv_bfloat16 *>(p.O) + (size_t)head * A.N * c : nullptr;
         float s[W];                                       // the state: row `row`, columns z0 ..
 #pragma unroll
@@ -296,146 +350,198 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             if (rows_y) {
 #pragma unroll
                 for (int q = 0; q < W / 8; ++q)
-                    *reinterpret_cast<uint4 *>(tile_chunk(sS, row, z0 / 8 + q)) =
-                        make_uint4(pack_bf16(s[8 * q], s[8 * q + 1]), pack_bf16(s[8 * q + 2], s[8 * q + 3]), pack_bf16(s[8 * q + 4], s[8 * q + 5]), pack_bf16(s[8 * q + 6], s[8 * q + 7]));
+                    sts16((sbase + M::S + own) ^ (q << 4), pack_bf16(s[8 * q], s[8 * q + 1]), pack_bf16(s[8 * q + 2], s[8 * q + 3]), pack_bf16(s[8 * q + 4], s[8 * q + 5]), pack_bf16(s[8 * q + 6], s[8 * q + 7]));
                 fence_async_smem();
             }
         };
         if (has0) put_state();
-        mbar_arrive_warp(bars + S_READY);
+        arrive_warp(bar + 8 * S_READY, lane);
         // A wait that gave up ends all further waiting, not the loop: the warps still meet at their barriers, on numbers that mean nothing.
         bool ok = true;
-#define DWAIT(bar, ph) do { if (ok) ok = wait_tries(bars + (bar), (ph), status, abort_flag); } while (0)
-        int Ltok = -1, inters = 0;
+#define DWAIT(b, ph) do { if (ok) ok = wait_tries(bar + 8 * (b), (ph), status); } while (0)
+        int Ltok = -1;
+        uint32_t inters = 0;
         // Brings item `it`'s weighted Y (of a chunk of L rows) into tensor memory.
         const auto prepare = [&](int it, int L) {
+            const uint32_t stage = sbase + (it & 1) * M::kStage;
             DWAIT(FULL0 + (it & 1), (it >> 1) & 1);
             if (L != Ltok || L < C) {
-                epi_sync();                               // the weights of the chunk before have been used
-                if (tid < C) tok[tid] = tid < L ? pw[reverse ? tid + 1 : L - 1 - tid] * p.tok_mul : 0.f;
+                warps_bar<32 * kWarps>();                 // the weights of the chunk before have been used
+                for (int i = tid; i < C; i += 32 * kWarps) {
+                    const float w = i < L ? pw[reverse ? i + 1 : L - 1 - i] * p.tok_mul : 0.f;
+                    if (whole) tok[i] = w;
+                    else {                                // pairs of tokens: the weights' first parts, then the second
+                        __nv_bfloat16 *at2 = reinterpret_cast<__nv_bfloat16 *>(tok) + (i >> 1) * 4 + (i & 1);
+                        at2[0] = __float2bfloat16_rn(w);
+                        at2[2] = __float2bfloat16_rn(w - __bfloat162float(at2[0]));
+                    }
+                }
                 if (L < C) {                              // rows behind the end are padding: zero, whatever they hold
-                    unsigned char *y = smem + (it & 1) * M::kStage + M::kX;
                     const int per = (M::kY + M::kZ) / 16384 * 8;      // chunks of 16 bytes of a row of Y and Z
-                    for (int i = tid; i < (C - L) * per; i += kEpiThreads) *reinterpret_cast<uint4 *>(tile_chunk(y, L + i / per, i % per)) = make_uint4(0, 0, 0, 0);
+                    for (int i = tid; i < (C - L) * per; i += 32 * kWarps) {
+                        const int r = L + i / per, q = i % per;
+                        sts16(stage + M::kX + (q >> 3) * 16384 + swz128(r, q & 7), 0, 0, 0, 0);
+                    }
                     fence_async_smem();
                 }
-                epi_sync();
-                if (L < C) mbar_arrive_warp(bars + CLEAN);
+                warps_bar<32 * kWarps>();
+                if (L < C) arrive_warp(bar + 8 * CLEAN, lane);
                 Ltok = L;
             }
-            if (rows_y) weighted_transpose<false>(smem_u32(smem + (it & 1) * M::kStage + M::kX), tok + cb * 32, at + kB + cb * 16, quarter, cb, lane);
-            if (MAIN && DZ == 128 && whole) return;         // the third part follows when the scores have been read
-            if (whole && rows_y) weighted_transpose<true>(smem_u32(smem + (it & 1) * M::kStage + M::kX), tok + cb * 32, at + kThird + cb * 16, quarter, cb, lane);
+            if (rows_y) {
+#pragma unroll
+                for (int tb = 0; tb < 4 / kGroups; ++tb) {
+                    const int t = cb + kGroups * tb;      // of 32 tokens
+                    const float *w = tok + t * 32 + 2 * (lane & 3);
+                    if (!whole) weighted_transpose<TWO>(stage + y_own + t * 4096, w, at + kB + t * 16, 0);
+                    else weighted_transpose<kBehindScores ? LEAD : ALL>(stage + y_own + t * 4096, w, at + kB + t * 16, at + kThird + t * 16);
+                }
+            }
+            if (kBehindScores && whole) return;           // the third part follows when the scores have been read
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive_warp(bars + T_READY);
+            arrive_warp(bar + 8 * T_READY, lane);
         };
         const auto rows_of = [&](int k) { return min(C, sp.n - first_row(k)); };
-        // P of a block off the diagonal: by column, and a power for the row, up to the block's near edge; on the diagonal by a table alone.
-        const bool off = reverse ? cb > quarter : cb < quarter;
-        const float p_row = off ? pw[reverse ? cb * 32 - row : row - cb * 32 - 31] : 1.f;
-        const float *p_col = off ? near : diag + (lane & 3) * kDiag + 32 - (lane & ~3);
+        // Blocks of 32 columns of the scores: one a warp of four, the outer or the inner two a warp of two (the triangle has as much in either).
+        // Off the diagonal by column, and a power for the row, up to the block's near edge; on the diagonal by a table alone.
+        const auto block_of = [&](int i) { return kGroups == 4 ? cb : cb == 0 ? 3 * i : 1 + i; };
+        float p_row[4 / kGroups];
+#pragma unroll
+        for (int i = 0; i < 4 / kGroups; ++i) {
+            const int blk = block_of(i);
+            p_row[i] = (reverse ? blk > quarter : blk < quarter) ? pw[reverse ? blk * 32 - row : row - blk * 32 - 31] : 1.f;
+        }
+        float x_row = 0.f;                                // of X S
+        int Lx = -1;
         if (items > 0) prepare(0, rows_of(0));
         for (int it = 0, k = 0, g = 0; it < items; ++it) {
             const int t0 = first_row(k), L = min(C, sp.n - t0);
             if (MAIN) {                                   // P: the lower (backwards: the upper) triangle, times the decays
                 DWAIT(SCORES, it & 1);
                 tc_fence_after();
-                uint32_t pk[16];
-                if (off || cb == quarter) {
-                    constexpr int kLd = DZ == 64 ? 32 : 16;      // (registers)
+                uint32_t pk[4 / kGroups][16];
 #pragma unroll
-                    for (int h = 0; h < 32; h += kLd) {
-                        uint32_t v[kLd];
-                        if constexpr (kLd == 32) tmem_ld32(at + kA + cb * 32, v);
-                        else tmem_ld16(at + kA + cb * 32 + h, v);
-                        tmem_wait_ld();
+                for (int i = 0; i < 4 / kGroups; ++i) {
+                    const int blk = block_of(i);
+                    const bool off = reverse ? blk > quarter : blk < quarter;
+                    if (off || blk == quarter) {
+                        const float *by = off ? near : diag + (lane & 3) * kDiag + 32 - (lane & ~3);
+                        constexpr int kLd = DZ == 64 || kGroups == 2 ? 32 : 16;      // (registers)
 #pragma unroll
-                        for (int j = 0; j < kLd; j += 4) {
-                            const float4 w = *reinterpret_cast<const float4 *>(p_col + h + j);
-                            float x[4] = {f(v[j]), f(v[j + 1]), f(v[j + 2]), f(v[j + 3])};
-                            mul2(x[0], x[1], p_row, p_row);
-                            mul2(x[2], x[3], p_row, p_row);
-                            mul2(x[0], x[1], w.x, w.y);
-                            mul2(x[2], x[3], w.z, w.w);
-                            pk[(h + j) / 2] = pack_bf16(x[0], x[1]);
-                            pk[(h + j) / 2 + 1] = pack_bf16(x[2], x[3]);
+                        for (int h = 0; h < 32; h += kLd) {
+                            uint32_t v[kLd];
+                            if constexpr (kLd == 32) tmem_ld32(at + kA + blk * 32, v);
+                            else tmem_ld16(at + kA + blk * 32 + h, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < kLd; j += 4) {
+                                const float4 w = *reinterpret_cast<const float4 *>(by + h + j);
+                                float x[4] = {f(v[j]), f(v[j + 1]), f(v[j + 2]), f(v[j + 3])};
+                                mul2(x[0], x[1], p_row[i], p_row[i]);
+                                mul2(x[2], x[3], p_row[i], p_row[i]);
+                                mul2(x[0], x[1], w.x, w.y);
+                                mul2(x[2], x[3], w.z, w.w);
+                                pk[i][(h + j) / 2] = pack_bf16(x[0], x[1]);
+                                pk[i][(h + j) / 2 + 1] = pack_bf16(x[2], x[3]);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) pk[i][j] = 0;
+                    }
+                }
+                quarter_bar<32 * kGroups>(quarter);       // P takes the place of scores that other warps read
+#pragma unroll
+                for (int i = 0; i < 4 / kGroups; ++i) tmem_st16(at + kA + block_of(i) * 16, pk[i]);
+                if (kBehindScores && whole) {
+                    if (rows_y) {
+#pragma unroll
+                        for (int tb = 0; tb < 4 / kGroups; ++tb) {
+                            const int t = cb + kGroups * tb;
+                            weighted_transpose<THIRD>(sbase + (it & 1) * M::kStage + y_own + t * 4096, tok + t * 32 + 2 * (lane & 3), 0, at + kThird + t * 16);
                         }
                     }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) pk[j] = 0;
-                }
-                quarter_sync(quarter);                    // P takes the place of scores that other warps read
-                tmem_st16(at + kA + cb * 16, pk);
-                if (DZ == 128 && whole) {
-                    if (rows_y) weighted_transpose<true>(smem_u32(smem + (it & 1) * M::kStage + M::kX), tok + cb * 32, at + kThird + cb * 16, quarter, cb, lane);
                     tmem_wait_st();
                     tc_fence_before();
-                    mbar_arrive_warp(bars + T_READY);
+                    arrive_warp(bar + 8 * T_READY, lane);
+                }
+                if (L != Lx) {
+                    x_row = row < L ? row_mul * pw[reverse ? L - 1 - row : row + 1] : 0.f;
+                    Lx = L;
                 }
                 if (DZ == 128 && g == 0 && (has0 || k > 0)) {
-                    DWAIT(INTER, inters & 1);
-                    ++inters;
+                    DWAIT(INTER, inters++ & 1);
                     tc_fence_after();
-                    uint32_t o[W];
-                    tmem_ld(at + kO + z0, o);
-                    tmem_wait_ld();
-                    const float r = row < L ? row_mul * pw[reverse ? L - 1 - row : row + 1] : 0.f;
 #pragma unroll
-                    for (int j = 0; j < W; ++j) o[j] = __float_as_uint(f(o[j]) * r);
-                    tmem_st(at + kO + z0, o);
+                    for (int h = 0; h < W; h += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(at + kO + z0 + h, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(f(o[j]) * x_row);
+                        tmem_st32(at + kO + z0 + h, o);
+                    }
                 }
                 tmem_wait_st();
                 tc_fence_before();
-                mbar_arrive_warp(bars + P_READY);
+                arrive_warp(bar + 8 * P_READY, lane);
             }
             DWAIT(DS, it & 1);
             if (g == G - 1) {
                 tc_fence_after();
-                uint32_t o[W];
-                tmem_ld(at + kD + z0, o);
-                tmem_wait_ld();
                 const float keep = pw[L];
+                constexpr int kLd = W < 32 ? W : 32;
 #pragma unroll
-                for (int j = 0; j < W; ++j) s[j] = fmaf(keep, s[j], f(o[j]));
+                for (int h = 0; h < W; h += kLd) {
+                    uint32_t o[kLd];
+                    tmem_ld<kLd>(at + kD + z0 + h, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < kLd; ++j) s[h + j] = fmaf(keep, s[h + j], f(o[j]));
+                }
                 if (MAIN) put_state();
                 tc_fence_before();
-                mbar_arrive_warp(bars + S_READY);
+                arrive_warp(bar + 8 * S_READY, lane);
             }
             if (MAIN) {
                 DWAIT(PZ, it & 1);
                 if (g == G - 1) {
                     tc_fence_after();
-                    uint32_t o[W];
-                    tmem_ld(at + kO + z0, o);
-                    if (DZ == 64 && (has0 || k > 0)) {
-                        uint32_t x[W];
-                        tmem_ld(at + kX + z0, x);
+                    constexpr int kLd = W < 32 ? W : 32;
+                    const uint32_t stage = sbase + (it & 1) * M::kStage + own;
+#pragma unroll
+                    for (int h = 0; h < W; h += kLd) {
+                        uint32_t o[kLd];
+                        tmem_ld<kLd>(at + kO + z0 + h, o);
+                        if (DZ == 64 && (has0 || k > 0)) {
+                            uint32_t x[kLd];
+                            tmem_ld<kLd>(at + kX + z0 + h, x);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < kLd; ++j) o[j] = __float_as_uint(fmaf(f(x[j]), x_row, f(o[j])));
+                        }
                         tmem_wait_ld();
-                        const float r = row < L ? row_mul * pw[reverse ? L - 1 - row : row + 1] : 0.f;
+                        if (h + kLd == W) {
+                            tc_fence_before();
+                            arrive_warp(bar + 8 * O_READ, lane);
+                        }
 #pragma unroll
-                        for (int j = 0; j < W; ++j) o[j] = __float_as_uint(fmaf(f(x[j]), r, f(o[j])));
+                        for (int q = 0; q < kLd / 8; ++q) {
+                            const uint4 r = pack8(o + 8 * q);
+                            if (L == C) sts16(stage ^ ((h / 8 + q) << 4), r.x, r.y, r.z, r.w);
+                            else if (row < L && z0 + h + 8 * q < c) *reinterpret_cast<uint4 *>(O + (size_t)(t0 + row) * c + z0 + h + 8 * q) = r;
+                        }
                     }
-                    tmem_wait_ld();
-                    tc_fence_before();
-                    mbar_arrive_warp(bars + O_READ);
-                    if (L == C) {
-#pragma unroll
-                        for (int q = 0; q < W / 8; ++q) *reinterpret_cast<uint4 *>(tile_chunk(smem + (it & 1) * M::kStage, row, z0 / 8 + q)) = pack8(o + 8 * q);
-                        fence_async_smem();
-                    } else if (row < L) {
-#pragma unroll
-                        for (int q = 0; q < W / 8; ++q)
-                            if (z0 + 8 * q < c) *reinterpret_cast<uint4 *>(O + (size_t)(t0 + row) * c + z0 + 8 * q) = pack8(o + 8 * q);
-                    }
-                    mbar_arrive_warp(bars + STAGED);
+                    fence_async_smem();
+                    arrive_warp(bar + 8 * STAGED, lane);
                 }
             }
             if (++g == G) { g = 0; ++k; }
             if (it + 1 < items) prepare(it + 1, rows_of(k));
         }
 #undef DWAIT
+        if (!ok) *abort_flag = 1;
         if (S_out && row < a) {
 #pragma unroll
             for (int j = 0; j < W; j += 4)
@@ -446,7 +552,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     if (*abort_flag) __nanosleep(200000);                 // copies that are still on their way
     tc_fence_before();
     __syncthreads();
-    if (warp == kEpiWarps) tmem_dealloc(tmem, 512);
+    if (warp == kWarps) tmem_dealloc(tmem, 512);
 }
 
 bool make_map3(CUtensorMap *m, const void *base, int heads, int N, int width)
