@@ -20,7 +20,7 @@ constexpr int C = 128;
 // Column groups: kGroups warps share a quarter of the rows, each takes DZ / kGroups columns of O, D and the state. Beside them one warp
 // loads and stores, one issues products.
 #ifndef NCOLS
-#define NCOLS 4
+#define NCOLS 2
 #endif
 constexpr int kGroups = NCOLS, kWarps = 4 * kGroups, kBlock = 32 * (kWarps + 2);
 static_assert(kGroups == 2 || kGroups == 4, "blocks of scores are shared out for these");
@@ -111,6 +111,12 @@ __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t 
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
     return d;
 }
+__device__ __forceinline__ uint32_t fms_bf16x2(uint32_t a, uint32_t b, uint32_t c)      // a b - c
+{
+    uint32_t d;
+    asm("{\n\t.reg .b32 n;\n\tneg.bf16x2 n, %3;\n\tfma.rn.bf16x2 %0, %1, %2, n;\n\t}" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+    return d;
+}
 // Four 8 x 8 matrices of 16-bit numbers, transposed: lane t receives of each the numbers 2 (t % 4) and the next of column t / 4.
 __device__ __forceinline__ void ldsm_t(uint32_t addr, uint32_t &r0, uint32_t &r1, uint32_t &r2, uint32_t &r3)
 {
@@ -151,7 +157,7 @@ __device__ __forceinline__ void weighted_transpose(uint32_t from, const float *w
             if (MODE == TWO) {
                 const uint32_t w1 = __float_as_uint(w[m >> 1].x), w2 = __float_as_uint(w[m >> 1].y);
                 p0[m] = mul_bf16x2(y[h][m], w1);
-                p1[m] = fma_bf16x2(y[h][m], w2, fma_bf16x2(y[h][m], w1, p0[m] ^ 0x80008000u));
+                p1[m] = fma_bf16x2(y[h][m], w2, fms_bf16x2(y[h][m], w1, p0[m]));
             } else {
                 float u = f(y[h][m] << 16), v = f(y[h][m] & 0xffff0000u);
                 mul2(u, v, w[m >> 1].x, w[m >> 1].y);
