@@ -26,7 +26,6 @@ constexpr int kGroups = NCOLS, kWarps = 4 * kGroups, kBlock = 32 * (kWarps + 2);
 static_assert(kGroups == 2 || kGroups == 4, "blocks of scores are shared out for these");
 constexpr uint32_t kA = 0, kB = 128, kO = 256, kD = 384; // columns of tensor memory
 constexpr uint32_t kX = 320;                             // X S of a narrow Z (64 columns), apart from P Z; of a wide one it goes to kO
-constexpr uint32_t kThirdWide = kA + 64, kThirdNarrow = 448;      // the third part of w Y: the half of the scores' columns that P does not take, or columns of its own
 constexpr int kDiag = 68;                                // numbers of each copy of the diagonal blocks' decays
 
 struct TcMaps { CUtensorMap x, y, z, o; };
@@ -136,7 +135,7 @@ __device__ __forceinline__ void tmem_st_16x128b(uint32_t a, const uint32_t (&v)[
 //              unpacking, a product in fp32 and taking it apart are 8 (the transposition of a chunk: 1100 cycles)
 //   LEAD       the first two of three parts, from an fp32 weight;  THIRD: the third;  ALL: three
 enum { TWO, LEAD, THIRD, ALL };
-template <int MODE>
+template <int MODE, uint32_t PART>
 __device__ __forceinline__ void weighted_transpose(uint32_t from, const float *weights, uint32_t to, uint32_t to3)
 {
     // from: the address of this lane's matrix row of the first 16 tokens and columns; 16 more columns are two 16-byte chunks (a swizzled bit) on
@@ -168,7 +167,7 @@ __device__ __forceinline__ void weighted_transpose(uint32_t from, const float *w
         }
         if (MODE != THIRD) {
             tmem_st_16x128b(to + lanes, p0);
-            tmem_st_16x128b(to + 64 + lanes, p1);
+            tmem_st_16x128b(to + PART + lanes, p1);
         }
         if (MODE >= THIRD) tmem_st_16x128b(to3 + lanes, p2);
     }
@@ -180,8 +179,14 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
 {
     using M = TcSmem<DY, DZ, MAIN>;
     constexpr int W = DZ / kGroups;                       // columns of O, D and the state a warp takes
-    constexpr uint32_t kThird = DZ == 64 ? kThirdNarrow : kThirdWide;
+    // Narrow tiles (64 x 64): a state has half the rows of tensor memory. The tokens' two halves take one half of the rows each, so that all
+    // warps transpose (with one half idle it was the longest step of a chunk), and leave two states, whose sum is the state: D is Y^T Z of the
+    // first 64 tokens in its upper left quarter, of the others in its lower right one, and X S is [X X] times both.
+    constexpr bool kHalves = DY == 64 && DZ == 64;
+    constexpr uint32_t kPart = kHalves ? 32 : 64;         // columns of a part of w Y
+    // the third part: behind the others, or in the half of the scores' columns that P does not take, once these have been read
     constexpr bool kBehindScores = MAIN && DZ == 128;
+    constexpr uint32_t kThird = kHalves ? kB + 64 : DZ == 64 ? 448 : kA + 64;
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char *sS = smem + M::S;
     float *tok = reinterpret_cast<float *>(smem + M::tok), *near = reinterpret_cast<float *>(smem + M::near), *diag = reinterpret_cast<float *>(smem + M::diag), *pw = reinterpret_cast<float *>(smem + M::pw);
@@ -283,7 +288,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         if (!ok) *abort_flag = 1;
     } else if (warp == kWarps + 1) {                   // ------------------------------------------------ products
         // In this order the pipe has something to do while the warps turn scores into P (X S, D), scale X S (D) and take the state (P Z).
-        const uint32_t id_scores = make_idesc(128, 128, 0, 0), id_z = make_idesc(128, DZ, 0, 1);
+        const uint32_t id_scores = make_idesc(128, 128, 0, 0), id_z = make_idesc(128, DZ, 0, 1), id_d = kHalves ? make_idesc(128, 128, 0, 1) : id_z;
         const TileDesc tS(sS);
         const int parts = whole ? 3 : 2;
         bool ok = true;
@@ -311,7 +316,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     tc_fence_after();
                     if (elect_one()) {
 #pragma unroll
-                        for (int q = 0; q < DY / 16; ++q) mma_ss(tmem + (DZ == 64 ? kX : kO), kdesc(tX, q), mndesc(tS, q), id_z, q > 0);
+                        for (int q = 0; q < (kHalves ? 8 : DY / 16); ++q)
+                            mma_ss(tmem + (DZ == 64 ? kX : kO), kdesc(tX, kHalves ? q & 3 : q), mndesc(tS, q), id_z, q > 0);
                         mma_commit(bars + INTER);
                     }
                 }
@@ -320,10 +326,12 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
+                const uint64_t halves = make_sdesc(smem_u32(stage + M::kX + M::kY), 64 * 128, 1024);      // Z's rows 0 .. 63 and 64 .. 127 as columns side by side
                 for (int part = 0; part < parts; ++part) {
-                    const uint32_t left = tmem + (part < 2 ? kB + 64 * part : kThird);
+                    const uint32_t left = tmem + (part < 2 ? kB + kPart * part : kThird);
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) mma_ts(tmem + kD, left + 8 * q, mndesc(tZ, q), id_z, g > 0 || part > 0 || q > 0);
+                    for (int q = 0; q < (kHalves ? 4 : 8); ++q)
+                        mma_ts(tmem + kD, left + 8 * q, kHalves ? halves + (uint64_t)(q * 2048 >> 4) : mndesc(tZ, q), id_d, g > 0 || part > 0 || q > 0);
                 }
                 mma_commit(bars + DS);
             }
@@ -342,15 +350,16 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     } else {                                              // ------------------------------------------------ what lies between the products
         const int quarter = warp & 3, cb = warp >> 2, row = quarter * 32 + lane, z0 = cb * W;
         const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16);
-        const bool rows_y = quarter * 32 < DY;            // this warp's lanes are rows of the state
+        const bool rows_y = kHalves || quarter * 32 < DY; // this warp's lanes are rows of the state
+        const int srow = kHalves ? row & 63 : row, half = kHalves ? quarter >> 1 : 0;      // row of the state, half of the tokens
         const uint32_t own = (uint32_t)((z0 >> 6) * 16384 + row * 128 + ((((z0 >> 3) & 7) ^ (row & 7)) << 4));      // this lane's first 16 bytes in a swizzled tile
-        const uint32_t y_own = (uint32_t)(M::kX + (quarter >> 1) * 16384 + (((lane >> 4) & 1) * 8 + (lane & 7)) * 128 + ((((quarter & 1) * 4 + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
+        const uint32_t y_own = (uint32_t)(M::kX + (kHalves ? half * 2 * 4096 : (quarter >> 1) * 16384) + (((lane >> 4) & 1) * 8 + (lane & 7)) * 128 + ((((quarter & 1) * 4 + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
         __nv_bfloat16 *O = MAIN ? static_cast<__nv_bfloat16 *>(p.O) + (size_t)head * A.N * c : nullptr;
         float s[W];                                       // the state: row `row`, columns z0 ..
 #pragma unroll
         for (int j = 0; j < W; ++j) {
             const int z = z0 + j;
-            s[j] = S_in && row < a && z < c ? (p.trans ? S_in[(size_t)z * a + row] : S_in[(size_t)row * c + z]) : 0.f;
+            s[j] = S_in && srow < a && z < c && half == 0 ? (p.trans ? S_in[(size_t)z * a + srow] : S_in[(size_t)srow * c + z]) : 0.f;
         }
         const auto put_state = [&]() {                    // its copy for the product with the next chunk's rows
             if (rows_y) {
@@ -396,11 +405,11 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             }
             if (rows_y) {
 #pragma unroll
-                for (int tb = 0; tb < 4 / kGroups; ++tb) {
+                for (int tb = 0; tb < (kHalves ? 2 : 4) / kGroups; ++tb) {
                     const int t = cb + kGroups * tb;      // of 32 tokens
-                    const float *w = tok + t * 32 + 2 * (lane & 3);
-                    if (!whole) weighted_transpose<TWO>(stage + y_own + t * 4096, w, at + kB + t * 16, 0);
-                    else weighted_transpose<kBehindScores ? LEAD : ALL>(stage + y_own + t * 4096, w, at + kB + t * 16, at + kThird + t * 16);
+                    const float *w = tok + (half * 2 + t) * 32 + 2 * (lane & 3);
+                    if (!whole) weighted_transpose<TWO, kPart>(stage + y_own + t * 4096, w, at + kB + t * 16, 0);
+                    else weighted_transpose<kBehindScores ? LEAD : ALL, kPart>(stage + y_own + t * 4096, w, at + kB + t * 16, at + kThird + t * 16);
                 }
             }
             if (kBehindScores && whole) return;           // the third part follows when the scores have been read
@@ -465,7 +474,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
 #pragma unroll
                         for (int tb = 0; tb < 4 / kGroups; ++tb) {
                             const int t = cb + kGroups * tb;
-                            weighted_transpose<THIRD>(sbase + (it & 1) * M::kStage + y_own + t * 4096, tok + t * 32 + 2 * (lane & 3), 0, at + kThird + t * 16);
+                            weighted_transpose<THIRD, kPart>(sbase + (it & 1) * M::kStage + y_own + t * 4096, tok + t * 32 + 2 * (lane & 3), 0, at + kThird + t * 16);
                         }
                     }
                     tmem_wait_st();
@@ -501,7 +510,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
 #pragma unroll
                 for (int h = 0; h < W; h += kLd) {
                     uint32_t o[kLd];
-                    tmem_ld<kLd>(at + kD + z0 + h, o);
+                    tmem_ld<kLd>(at + kD + half * 64 + z0 + h, o);
                     tmem_wait_ld();
 #pragma unroll
                     for (int j = 0; j < kLd; ++j) s[h + j] = fmaf(keep, s[h + j], f(o[j]));
@@ -548,10 +557,30 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         }
 #undef DWAIT
         if (!ok) *abort_flag = 1;
-        if (S_out && row < a) {
+        if (S_out) {
+            if (kHalves) {                                // the other half's state: where the copy was, or (states alone) in a stage, 16 KB
+                const uint32_t at2 = sbase + (MAIN ? M::S : 0);
+                const auto cell = [&](int j) { return at2 + (uint32_t)((srow * 16 + ((z0 + j) / 4 ^ (srow & 15))) * 16); };
+                warps_bar<32 * kWarps>();                 // the last copies have been written
+                if (half == 1) {
 #pragma unroll
-            for (int j = 0; j < W; j += 4)
-                if (z0 + j < c) *reinterpret_cast<float4 *>(S_out + (size_t)row * c + z0 + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+                    for (int j = 0; j < W; j += 4) sts16(cell(j), __float_as_uint(s[j]), __float_as_uint(s[j + 1]), __float_as_uint(s[j + 2]), __float_as_uint(s[j + 3]));
+                }
+                warps_bar<32 * kWarps>();
+                if (half == 0) {
+#pragma unroll
+                    for (int j = 0; j < W; j += 4) {
+                        float4 x;
+                        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(cell(j)) : "memory");
+                        s[j] += x.x; s[j + 1] += x.y; s[j + 2] += x.z; s[j + 3] += x.w;
+                    }
+                }
+            }
+            if (half == 0 && srow < a) {
+#pragma unroll
+                for (int j = 0; j < W; j += 4)
+                    if (z0 + j < c) *reinterpret_cast<float4 *>(S_out + (size_t)srow * c + z0 + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+            }
         }
     }
     __syncwarp();
