@@ -22,7 +22,7 @@ struct DecayPass {
     void *O;                    // [B, HX, N, c]
     const float *S_in;          // state the pass enters by, [B, Hkv, d, dv]; null: zero
     float *S_out;               // state it leaves by; null: not wanted (always null where trans is set)
-    const float *seg;           // states the segments behind the first enter by, [B * Hkv, nseg - 1, d, dv]
+    const float *seg;           // states the pieces behind the first enter by, [B * Hkv, (nseg - 1) sub, d, dv]
     int a, c;
     int HX, HY;                 // heads of X and O, and of Y and Z: where HX > HY consecutive heads of X share one of Y, where
                                 // HY > HX the sum runs over consecutive heads of Y
@@ -41,7 +41,9 @@ struct DecayArgs {
     const int *lengths;         // [B] or null
     int B, Hkv, N;
     int nseg, cps;              // segments of a sequence, chunks of each
+    int sub;                    // pieces that each of the first nseg - 1 segments is cut into where their states are summed
     int *status;
+    int clear;                  // the call's first kernel: sets the status to zero
 };
 
 // Segments are counted in the order the pass takes the chunks: its k-th chunk is chunk k forwards, T - 1 - k backwards.
@@ -72,7 +74,7 @@ struct darkattn_decay_layout {
 struct darkattn_decay_plan_s {
     darkattn_decay_desc_t desc;
     int path;
-    struct { int nseg, cps; } fwd, bwd;
+    struct { int nseg, cps, sub; } fwd, bwd;
     darkattn::darkattn_decay_layout ws;
     size_t workspace_bytes;
 };
@@ -82,8 +84,19 @@ namespace darkattn {
 // FP32 kernels, any shape
 void decay_simt_split(darkattn_decay_plan_s *plan);
 darkattn_status_t decay_simt_run(DecayArgs &A, DecayPass *state_pass, int nstate, int bf16, cudaStream_t st);
-// Adds up the segments' states in place: slot s then holds the state that segment s + 1 enters by.
-cudaError_t decay_scan_segments(const DecayArgs &A, const DecayPass &p, int chunk, cudaStream_t st);
+// The arguments of the kernels that sum the states of the pieces: segments of cps / sub chunks, all but the last summed.
+inline DecayArgs decay_pieces(const DecayArgs &A, const DecayPass *pass, int npass)
+{
+    DecayArgs P = A;
+    P.npass = npass;
+    for (int i = 0; i < npass; ++i) P.pass[i] = pass[i];
+    P.nseg = (A.nseg - 1) * A.sub + 1;
+    P.cps = A.cps / A.sub;
+    P.sub = 1;
+    return P;
+}
+// Adds up the pieces' states in place: slot s then holds the state that piece s + 1 enters by.
+cudaError_t decay_scan_pieces(const DecayArgs &P, const DecayPass &p, int chunk, cudaStream_t st);
 
 // tcgen05 kernels, bf16
 bool decay_tc_supported(const darkattn_decay_desc_t &ds);

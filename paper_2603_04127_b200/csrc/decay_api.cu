@@ -33,13 +33,13 @@ __global__ void __launch_bounds__(256) decay_zero_tail_kernel(unsigned char *dQ,
     }
 }
 
-static DecayArgs common_args(const darkattn_decay_plan_s *plan, const float *log_decay, const int *lengths, int nseg, int cps, void *ws)
+static DecayArgs common_args(const darkattn_decay_plan_s *plan, const float *log_decay, const int *lengths, int nseg, int cps, int sub, void *ws)
 {
     DecayArgs A = {};
     A.log_decay = log_decay;
     A.lengths = lengths;
     A.B = plan->desc.B; A.Hkv = plan->desc.H_kv; A.N = plan->desc.N;
-    A.nseg = nseg; A.cps = cps;
+    A.nseg = nseg; A.cps = cps; A.sub = sub;
     A.status = static_cast<int *>(ws);
     return A;
 }
@@ -79,9 +79,9 @@ darkattn_status_t darkattn_decay_plan(const darkattn_decay_desc_t *desc, darkatt
     p->path = ds.path == DARKATTN_PATH_AUTO ? (tensor_ok ? DARKATTN_PATH_TENSOR : DARKATTN_PATH_SIMT) : ds.path;
     if (p->path == DARKATTN_PATH_TENSOR) decay_tc_split(p);
     else decay_simt_split(p);
-    // states of the segments: one set forwards, for a backward pass one more
+    // states of the pieces: one set forwards, for a backward pass one more
     const size_t set = (size_t)ds.B * ds.H_kv * ds.d * ds.dv * sizeof(float);
-    const size_t nf = set * (p->fwd.nseg - 1), nb = set * (p->bwd.nseg - 1);
+    const size_t nf = set * ((p->fwd.nseg - 1) * p->fwd.sub), nb = set * ((p->bwd.nseg - 1) * p->bwd.sub);
     p->ws.status = 0;
     p->ws.seg[0] = 256;
     p->ws.seg[1] = 256 + ((nb + 255) & ~(size_t)255);
@@ -104,7 +104,7 @@ darkattn_status_t darkattn_decay_forward(darkattn_decay_plan_t plan, const void 
     const darkattn_decay_desc_t &ds = plan->desc;
     if (overlap(S_in, S_out, (size_t)ds.B * ds.H_kv * ds.d * ds.dv * sizeof(float))) return DARKATTN_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    DecayArgs A = common_args(plan, log_decay, lengths, plan->fwd.nseg, plan->fwd.cps, workspace);
+    DecayArgs A = common_args(plan, log_decay, lengths, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub, workspace);
     float *seg = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->ws.seg[0]);
     A.npass = 1;
     A.pass[0] = DecayPass{Q, K, V, O, S_in, S_out, seg, ds.d, ds.dv, ds.H, ds.H_kv, 0, 0, ds.scale, ds.scale, 1.f, S_out != nullptr};
@@ -123,7 +123,7 @@ darkattn_status_t darkattn_decay_backward(darkattn_decay_plan_t plan, const void
     const size_t states = (size_t)ds.B * ds.H_kv * ds.d * ds.dv * sizeof(float);
     if (overlap(dS_out, dS_in, states) || overlap(S_in, dS_in, states)) return DARKATTN_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    DecayArgs A = common_args(plan, log_decay, lengths, plan->bwd.nseg, plan->bwd.cps, workspace);
+    DecayArgs A = common_args(plan, log_decay, lengths, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub, workspace);
     float *S = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->ws.seg[0]), *R = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->ws.seg[1]);
     A.npass = 3;
     A.pass[0] = DecayPass{dO, V, K, dQ, S_in, nullptr, S, ds.dv, ds.d, ds.H, ds.H_kv, 0, 1, ds.scale, ds.scale, 1.f, 0};

@@ -80,7 +80,7 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
 
     if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
     const float *S_in = nullptr;
-    if (MAIN) S_in = seg == 0 ? (p.S_in ? p.S_in + (size_t)(b * A.Hkv + hs) * a * c : nullptr) : p.seg + ((size_t)(b * A.Hkv + hs) * (nseg - 1) + seg - 1) * a * c;
+    if (MAIN) S_in = seg == 0 ? (p.S_in ? p.S_in + (size_t)(b * A.Hkv + hs) * a * c : nullptr) : p.seg + ((size_t)(b * A.Hkv + hs) * (nseg - 1) * A.sub + seg * A.sub - 1) * a * c;
     for (int i = tid; i < nf * F * TZ; i += kThreadsS) {
         const int f = i / TZ, z = z0 + i % TZ;
         S[i] = S_in && f < a && z < c ? (p.trans ? S_in[(size_t)z * a + f] : S_in[(size_t)f * c + z]) : 0.f;
@@ -184,16 +184,18 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
 __global__ void __launch_bounds__(256) decay_scan_kernel(const __grid_constant__ DecayArgs A, const __grid_constant__ DecayPass p, int chunk)
 {
     pdl_wait();
+    __shared__ float power[2];
     const int size = p.a * p.c, i = blockIdx.x * 256 + threadIdx.x, hs = blockIdx.y % A.Hkv, b = blockIdx.y / A.Hkv;
-    if (i >= size) return;
     int n = A.N;
     if (A.lengths) n = min(max(A.lengths[b], 0), A.N);
     const int T = (n + chunk - 1) / chunk;
-    const float g = A.log_decay[hs];
-    const float whole = decay_power(g, A.cps * chunk), first = p.reverse ? decay_power(g, A.cps * chunk - (T * chunk - n)) : whole;
+    if (threadIdx.x < 2) power[threadIdx.x] = decay_power(A.log_decay[hs], A.cps * chunk - (threadIdx.x && p.reverse ? T * chunk - n : 0));
+    __syncthreads();
+    if (i >= size) return;
+    const float whole = power[0], first = power[1];
     float s = p.S_in ? p.S_in[(size_t)blockIdx.y * size + i] : 0.f;
     float *at = const_cast<float *>(p.seg) + (size_t)blockIdx.y * (A.nseg - 1) * size + i;
-#pragma unroll 4
+#pragma unroll 8
     for (int k = 0; k + 1 < A.nseg; ++k) {
         if ((k + 1) * A.cps >= T) break;                     // the next segment has no chunk
         s = (k == 0 ? first : whole) * s + at[(size_t)k * size];
@@ -224,7 +226,7 @@ cudaError_t launch_t(const DecayArgs &A, cudaStream_t st)
 
 }  // namespace
 
-cudaError_t decay_scan_segments(const DecayArgs &A, const DecayPass &p, int chunk, cudaStream_t st)
+cudaError_t decay_scan_pieces(const DecayArgs &A, const DecayPass &p, int chunk, cudaStream_t st)
 {
     return launch_pdl(decay_scan_kernel, dim3((unsigned)((p.a * p.c + 255) / 256), (unsigned)(A.B * A.Hkv)), dim3(256), 0, st, A, p, chunk);
 }
@@ -246,11 +248,9 @@ static cudaError_t run_main(const DecayArgs &A, int bf16, cudaStream_t st)
 darkattn_status_t decay_simt_run(DecayArgs &A, DecayPass *state_pass, int nstate, int bf16, cudaStream_t st)
 {
     if (A.nseg > 1) {
-        DecayArgs P = A;
-        P.npass = nstate;
-        for (int i = 0; i < nstate; ++i) P.pass[i] = state_pass[i];
+        const DecayArgs P = decay_pieces(A, state_pass, nstate);
         DARKATTN_CUDA_TRY((bf16 ? launch_t<__nv_bfloat16, false>(P, st) : launch_t<float, false>(P, st)), "decay_simt_kernel (states)");
-        for (int i = 0; i < nstate; ++i) DARKATTN_CUDA_TRY(decay_scan_segments(A, state_pass[i], C, st), "decay_scan_kernel");
+        for (int i = 0; i < nstate; ++i) DARKATTN_CUDA_TRY(decay_scan_pieces(P, state_pass[i], C, st), "decay_scan_kernel");
     }
     DARKATTN_CUDA_TRY(run_main(A, bf16, st), "decay_simt_kernel");
     return DARKATTN_OK;
@@ -258,9 +258,10 @@ darkattn_status_t decay_simt_run(DecayArgs &A, DecayPass *state_pass, int nstate
 
 // Segments: as many as shorten the longest chain of chunks by more than the states' own pass and the sum over them cost. In units of a
 // chunk's time; a chunk of the states' pass is one product of four.
-static void pick(int T, long long units, long long state_units, int slots, int &nseg, int &cps)
+static void pick(int T, long long units, long long state_units, int slots, int &nseg, int &cps, int &sub)
 {
     double best = 1e30;
+    sub = 1;
     for (int n = 1; n <= T && n <= 128; ++n) {
         const int per = (T + n - 1) / n, m = (T + per - 1) / per;
         double cost = (double)((units * m + slots - 1) / slots) * (per + 1);
@@ -276,8 +277,8 @@ void decay_simt_split(darkattn_decay_plan_s *plan)
     const int tz = w <= 128 && w > 64 ? 128 : 64;
     const long long zf = (ds.dv + tz - 1) / tz, zb = (w + tz - 1) / tz;
     const int slots = w <= 64 ? 296 : 148;
-    pick(T, (long long)ds.B * ds.H * zf, (long long)ds.B * ds.H_kv * zf, slots, plan->fwd.nseg, plan->fwd.cps);
-    pick(T, (long long)ds.B * (ds.H + 2 * ds.H) * zb, 2LL * ds.B * ds.H * zf, slots, plan->bwd.nseg, plan->bwd.cps);
+    pick(T, (long long)ds.B * ds.H * zf, (long long)ds.B * ds.H_kv * zf, slots, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub);
+    pick(T, (long long)ds.B * (ds.H + 2 * ds.H) * zb, 2LL * ds.B * ds.H * zf, slots, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub);
 }
 
 }  // namespace darkattn

@@ -220,6 +220,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     tc_fence_after();
     pdl_wait_tma();
     const uint32_t tmem = uniform(*tmem_slot);
+    // (The first block to start clears the status; a wait gives up milliseconds later.)
+    if (A.clear && blockIdx.x == 0 && tid == 0) *A.status = 0;
 
     const int b = head / HX, hx = head % HX, hs = hx / (HX / A.Hkv);
     const int G = p.HY > HX ? p.HY / HX : 1;              // heads of Y that are summed over
@@ -234,11 +236,29 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     const float *S_in = nullptr;
     float *S_out = nullptr;
     if (MAIN) {
-        S_in = seg == 0 ? (p.S_in ? p.S_in + state : nullptr) : p.seg + ((size_t)(b * A.Hkv + hs) * (nseg - 1) + seg - 1) * a * c;
+        S_in = seg == 0 ? (p.S_in ? p.S_in + state : nullptr) : p.seg + ((size_t)(b * A.Hkv + hs) * (nseg - 1) * A.sub + seg * A.sub - 1) * a * c;
         if (p.S_out && last_seg && hx % (HX / A.Hkv) == 0) S_out = p.S_out + state;
     } else if (nchunk) S_out = const_cast<float *>(p.seg) + ((size_t)(b * A.Hkv + hs) * nseg + seg) * a * c;
     const bool has0 = MAIN && S_in != nullptr;
     const bool whole = MAIN ? S_out != nullptr : p.whole;   // three parts
+    const auto first_row = [&](int k) { return (reverse ? sp.T - 1 - (sp.k0 + k) : sp.k0 + k) * C; };
+    const auto load = [&](int it, int k, int g) {         // item `it`: chunk k, head g of those summed over
+        if (elect_one()) {
+            const TcMaps &m = P.m[ip];
+            unsigned char *stage = smem + (it & 1) * M::kStage;
+            const int t0 = first_row(k), hy = hy0 + g;
+            uint64_t *full = bars + FULL0 + (it & 1);
+            mbar_expect_tx(full, M::kStage);
+            if (MAIN) for (int x = 0; x < DY; x += 64) load3(stage + x * 256, &m.x, full, x, t0, head);
+            for (int x = 0; x < DY; x += 64) load3(stage + M::kX + x * 256, &m.y, full, x, t0, hy);
+            for (int x = 0; x < DZ; x += 64) load3(stage + M::kX + M::kY + x * 256, &m.z, full, x, t0, hy);
+        }
+    };
+    const bool fine = *abort_flag == 0;
+    if (warp == kWarps && fine) {                         // the first two items' loads, beside the tables
+        if (items > 0) load(0, 0, 0);
+        if (items > 1) load(1, G == 1, G == 1 ? 0 : 1);
+    }
     if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
     __syncthreads();
     // Decays of a block of 32 x 32 scores by column, times p_mul: from the near edge where the block is off the diagonal; on it, where row r needs
@@ -250,10 +270,9 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     }
     __syncthreads();
 
-    const auto first_row = [&](int k) { return (reverse ? sp.T - 1 - (sp.k0 + k) : sp.k0 + k) * C; };
     int *status = A.status;
 
-    if (*abort_flag) {
+    if (!fine) {
         if (tid == 0) atomicExch(status, (int)DARKATTN_ERR_CUDA);
     } else if (warp == kWarps) {                       // ------------------------------------------------ loads and stores
         const TcMaps &m = P.m[ip];
@@ -273,14 +292,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 if (++g2 == G) { g2 = 0; ++k2; }
             }
             if (it < items) {
-                if (elect_one()) {
-                    const int t0 = first_row(k), hy = hy0 + g;
-                    uint64_t *full = bars + FULL0 + (it & 1);
-                    mbar_expect_tx(full, M::kStage);
-                    if (MAIN) for (int x = 0; x < DY; x += 64) load3(stage + x * 256, &m.x, full, x, t0, head);
-                    for (int x = 0; x < DY; x += 64) load3(stage + M::kX + x * 256, &m.y, full, x, t0, hy);
-                    for (int x = 0; x < DZ; x += 64) load3(stage + M::kX + M::kY + x * 256, &m.z, full, x, t0, hy);
-                }
+                if (it >= 2) load(it, k, g);
                 if (++g == G) { g = 0; ++k; }
             }
         }
@@ -611,7 +623,7 @@ cudaError_t launch(const TcArgs &P, cudaStream_t st)
 
 // passes whose widths are of one class share a launch
 template <bool MAIN>
-darkattn_status_t launch_all(const DecayArgs &A, const DecayPass *pass, int npass, cudaStream_t st)
+darkattn_status_t launch_all(const DecayArgs &A, const DecayPass *pass, int npass, bool first, cudaStream_t st)
 {
     bool done[kDecayPasses] = {};
     for (int i = 0; i < npass; ++i) {
@@ -619,6 +631,7 @@ darkattn_status_t launch_all(const DecayArgs &A, const DecayPass *pass, int npas
         const bool y2 = pass[i].a > 64, z2 = pass[i].c > 64;
         TcArgs P;
         P.a = A;
+        P.a.clear = first && i == 0;
         int n = 0;
         for (int j = i; j < npass; ++j) {
             const DecayPass &q = pass[j];
@@ -645,34 +658,41 @@ bool decay_tc_supported(const darkattn_decay_desc_t &ds)
     return ds.dtype == DARKATTN_BF16 && ds.d % 8 == 0 && ds.dv % 8 == 0 && ds.d <= 128 && ds.dv <= 128;
 }
 
-// As for the FP32 kernels; in units of a chunk's time, one block an SM.
-static void pick(int T, long long units, long long state_units, int &nseg, int &cps)
+// Segments, and the pieces whose states are summed first.
+static void pick(int T, long long units, long long state_units, int &nseg, int &cps, int &sub)
 {
+    nseg = 1; cps = T; sub = 1;
     double best = 1e30;
-    for (int n = 1; n <= T && n <= 128; ++n) {
-        const int per = (T + n - 1) / n, m = (T + per - 1) / per;
-        double cost = (double)((units * m + 147) / 148) * (per + 1.5);
-        if (m > 1) cost += (double)((state_units * (m - 1) + 147) / 148) * (0.6 * per + 1.5) + 2 + 0.1 * m;
-        if (cost < best) { best = cost; nseg = m; cps = per; }
+    for (int n = 1; n <= T && n <= 64; ++n) {
+        for (int q = 1; q <= 4; ++q) {
+            const int per = ((T + n - 1) / n + q - 1) / q * q, m = (T + per - 1) / per;
+            double cost = (double)((units * m + 147) / 148) * (per + 1.5);
+            if (m > 1) cost += (double)((state_units * (m - 1) * q + 147) / 148) * (0.6 * per / q + 1.5) + 2 + 0.1 * m * q;
+            else if (q > 1) continue;
+            if (cost < best) { best = cost; nseg = m; cps = per; sub = q; }
+        }
     }
+#ifdef FORCE
+    if (getenv("NSEG")) { int n = atoi(getenv("NSEG")), q = atoi(getenv("SUB")); cps = ((T + n - 1) / n + q - 1) / q * q; nseg = (T + cps - 1) / cps; sub = q; }
+#endif
 }
 
 void decay_tc_split(darkattn_decay_plan_s *plan)
 {
     const darkattn_decay_desc_t &ds = plan->desc;
     const int T = (ds.N + C - 1) / C;
-    pick(T, (long long)ds.B * ds.H, (long long)ds.B * ds.H_kv, plan->fwd.nseg, plan->fwd.cps);
-    pick(T, 3LL * ds.B * ds.H, 2LL * ds.B * ds.H, plan->bwd.nseg, plan->bwd.cps);
+    pick(T, (long long)ds.B * ds.H, (long long)ds.B * ds.H_kv, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub);
+    pick(T, 3LL * ds.B * ds.H, 2LL * ds.B * ds.H, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub);
 }
 
 darkattn_status_t decay_tc_run(DecayArgs &A, DecayPass *state_pass, int nstate, cudaStream_t st)
 {
-    DARKATTN_CUDA_TRY(cudaMemsetAsync(A.status, 0, sizeof(int), st), "decay: status");
     if (A.nseg > 1) {
-        if (darkattn_status_t rc = launch_all<false>(A, state_pass, nstate, st)) return rc;
-        for (int i = 0; i < nstate; ++i) DARKATTN_CUDA_TRY(decay_scan_segments(A, state_pass[i], C, st), "decay_scan_kernel");
+        const DecayArgs P = decay_pieces(A, state_pass, nstate);
+        if (darkattn_status_t rc = launch_all<false>(P, P.pass, nstate, true, st)) return rc;
+        for (int i = 0; i < nstate; ++i) DARKATTN_CUDA_TRY(decay_scan_pieces(P, state_pass[i], C, st), "decay_scan_kernel");
     }
-    return launch_all<true>(A, A.pass, A.npass, st);
+    return launch_all<true>(A, A.pass, A.npass, A.nseg == 1, st);
 }
 
 }  // namespace darkattn
