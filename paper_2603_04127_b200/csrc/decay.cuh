@@ -95,8 +95,9 @@ inline DecayArgs decay_pieces(const DecayArgs &A, const DecayPass *pass, int npa
     P.sub = 1;
     return P;
 }
-// Adds up the pieces' states in place: slot s then holds the state that piece s + 1 enters by.
-cudaError_t decay_scan_pieces(const DecayArgs &P, const DecayPass &p, int chunk, cudaStream_t st);
+// Adds up the pieces' states in place: slot s then holds the state that piece s + 1 enters by. `by4`: a slot's numbers lie as
+// [dv / 4][d][4] (what a warp with a row a lane reads and writes 16 bytes at a time is contiguous), else as [d][dv].
+cudaError_t decay_scan_pieces(const DecayArgs &P, const DecayPass &p, int chunk, bool by4, cudaStream_t st);
 
 // tcgen05 kernels, bf16
 bool decay_tc_supported(const darkattn_decay_desc_t &ds);

@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
 
 // One thread per element of the state, along the segments. Tokens of segment s: whole chunks, but for a pass backwards, whose first
 // chunk may be a short one.
-__global__ void __launch_bounds__(256) decay_scan_kernel(const __grid_constant__ DecayArgs A, const __grid_constant__ DecayPass p, int chunk)
+__global__ void __launch_bounds__(256) decay_scan_kernel(const __grid_constant__ DecayArgs A, const __grid_constant__ DecayPass p, int chunk, int by4)
 {
     pdl_wait();
     __shared__ float power[2];
@@ -193,13 +193,21 @@ __global__ void __launch_bounds__(256) decay_scan_kernel(const __grid_constant__
     __syncthreads();
     if (i >= size) return;
     const float whole = power[0], first = power[1];
-    float s = p.S_in ? p.S_in[(size_t)blockIdx.y * size + i] : 0.f;
+    const int from = by4 ? i / 4 % p.a * p.c + i / 4 / p.a * 4 + i % 4 : i;
+    float s = p.S_in ? p.S_in[(size_t)blockIdx.y * size + from] : 0.f;
     float *at = const_cast<float *>(p.seg) + (size_t)blockIdx.y * (A.nseg - 1) * size + i;
-#pragma unroll 8
-    for (int k = 0; k + 1 < A.nseg; ++k) {
-        if ((k + 1) * A.cps >= T) break;                     // the next segment has no chunk
-        s = (k == 0 ? first : whole) * s + at[(size_t)k * size];
-        at[(size_t)k * size] = s;
+    const int n_at = min(A.nseg - 1, (T + A.cps - 1) / A.cps - 1);      // pieces that another with a chunk follows
+    constexpr int kAhead = 8;                                // loads on their way together (a piece at a time took 0.3 us each)
+    for (int k0 = 0; k0 < n_at; k0 += kAhead) {
+        float x[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) x[j] = k0 + j < n_at ? at[(size_t)(k0 + j) * size] : 0.f;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (k0 + j < n_at) {
+                s = (k0 + j == 0 ? first : whole) * s + x[j];
+                at[(size_t)(k0 + j) * size] = s;
+            }
     }
 }
 
@@ -226,9 +234,9 @@ cudaError_t launch_t(const DecayArgs &A, cudaStream_t st)
 
 }  // namespace
 
-cudaError_t decay_scan_pieces(const DecayArgs &A, const DecayPass &p, int chunk, cudaStream_t st)
+cudaError_t decay_scan_pieces(const DecayArgs &A, const DecayPass &p, int chunk, bool by4, cudaStream_t st)
 {
-    return launch_pdl(decay_scan_kernel, dim3((unsigned)((p.a * p.c + 255) / 256), (unsigned)(A.B * A.Hkv)), dim3(256), 0, st, A, p, chunk);
+    return launch_pdl(decay_scan_kernel, dim3((unsigned)((p.a * p.c + 255) / 256), (unsigned)(A.B * A.Hkv)), dim3(256), 0, st, A, p, chunk, (int)by4);
 }
 
 // passes of equal numbers of heads share a launch
@@ -250,7 +258,7 @@ darkattn_status_t decay_simt_run(DecayArgs &A, DecayPass *state_pass, int nstate
     if (A.nseg > 1) {
         const DecayArgs P = decay_pieces(A, state_pass, nstate);
         DARKATTN_CUDA_TRY((bf16 ? launch_t<__nv_bfloat16, false>(P, st) : launch_t<float, false>(P, st)), "decay_simt_kernel (states)");
-        for (int i = 0; i < nstate; ++i) DARKATTN_CUDA_TRY(decay_scan_pieces(P, state_pass[i], C, st), "decay_scan_kernel");
+        for (int i = 0; i < nstate; ++i) DARKATTN_CUDA_TRY(decay_scan_pieces(P, state_pass[i], C, false, st), "decay_scan_kernel");
     }
     DARKATTN_CUDA_TRY(run_main(A, bf16, st), "decay_simt_kernel");
     return DARKATTN_OK;

@@ -368,10 +368,20 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         const uint32_t y_own = (uint32_t)(M::kX + (kHalves ? half * 2 * 4096 : (quarter >> 1) * 16384) + (((lane >> 4) & 1) * 8 + (lane & 7)) * 128 + ((((quarter & 1) * 4 + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
         __nv_bfloat16 *O = MAIN ? static_cast<__nv_bfloat16 *>(p.O) + (size_t)head * A.N * c : nullptr;
         float s[W];                                       // the state: row `row`, columns z0 ..
+        const bool by4 = MAIN && seg > 0;                 // between segments as [dv / 4][d][4], from the caller as [d][dv]
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
+        for (int j = 0; j < W; j += 4) {
+            float4 x = make_float4(0, 0, 0, 0);
             const int z = z0 + j;
-            s[j] = S_in && srow < a && z < c && half == 0 ? (p.trans ? S_in[(size_t)z * a + srow] : S_in[(size_t)srow * c + z]) : 0.f;
+            if (S_in && srow < a && z < c && half == 0) {
+                if (!p.trans) x = *reinterpret_cast<const float4 *>(S_in + (by4 ? ((size_t)(z / 4) * a + srow) * 4 : (size_t)srow * c + z));
+                else {                                    // rows here are columns there; z and the three behind it are rows
+                    const float *col = S_in + (by4 ? ((size_t)(srow / 4) * c + z) * 4 + srow % 4 : (size_t)z * a + srow);
+                    const int step = by4 ? 4 : a;
+                    x = make_float4(col[0], col[step], col[2 * step], col[3 * step]);
+                }
+            }
+            s[j] = x.x; s[j + 1] = x.y; s[j + 2] = x.z; s[j + 3] = x.w;
         }
         const auto put_state = [&]() {                    // its copy for the product with the next chunk's rows
             if (rows_y) {
@@ -591,7 +601,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             if (half == 0 && srow < a) {
 #pragma unroll
                 for (int j = 0; j < W; j += 4)
-                    if (z0 + j < c) *reinterpret_cast<float4 *>(S_out + (size_t)srow * c + z0 + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+                    if (z0 + j < c) *reinterpret_cast<float4 *>(S_out + (MAIN ? (size_t)srow * c + z0 + j : ((size_t)((z0 + j) / 4) * a + srow) * 4)) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
             }
         }
     }
@@ -658,17 +668,28 @@ bool decay_tc_supported(const darkattn_decay_desc_t &ds)
     return ds.dtype == DARKATTN_BF16 && ds.d % 8 == 0 && ds.dv % 8 == 0 && ds.d <= 128 && ds.dv <= 128;
 }
 
-// Segments, and the pieces whose states are summed first.
-static void pick(int T, long long units, long long state_units, int &nseg, int &cps, int &sub)
+// Segments, and the pieces whose states are summed first: the cheapest by an estimate in us, fitted to measurements on a B200. A chunk takes 2.6 us
+// (wide tiles, 64 to 128 columns) or 1.7 us while few blocks run, and what the memory gives when all SMs do (5.7 and, power-bound, 4.8 TB/s);
+// a chunk of the states alone 1.4 or 1.0 us; two kernels more 13 or 6 us, twice that where there are two sets of states. One head of 8192 tokens, d 128: 178 us in one
+// segment, 31 in 32; 4 x 16 heads: 164 in one, 139 in two with two pieces each, 188 in four; 8 heads of 65536, d 64: 113 in 18.
+// Segments have to promise 8 % (a backward pass in one segment shares more of its reads in L2 than the estimate knows: 4 x 16 heads, 337 us
+// in one, 359 in two).
+static void pick(int T, int d, int dv, long long units, long long state_units, int sets, int &nseg, int &cps, int &sub)
 {
+    const bool wide = d > 64 || dv > 64;
+    const double chunk = wide ? 2.6 : 1.7, state_chunk = wide ? 1.4 : 1.0, more = sets * (wide ? 13 : 6), rate = wide ? 5.7e6 : 4.8e6;
+    const double bytes = 2.0 * C * 2 * (d + dv);
+    const auto phase = [&](long long blocks, int per, double us, double b) {
+        const double all = 148 * b / rate, rest = (double)(blocks % 148) * b / rate;
+        return per * ((double)(blocks / 148) * (all > us ? all : us) + (blocks % 148 ? (rest > us ? rest : us) : 0));
+    };
     nseg = 1; cps = T; sub = 1;
-    double best = 1e30;
-    for (int n = 1; n <= T && n <= 64; ++n) {
+    double best = phase(units, T, chunk, bytes);
+    for (int n = 2; n <= T && n <= 64; ++n) {
         for (int q = 1; q <= 4; ++q) {
             const int per = ((T + n - 1) / n + q - 1) / q * q, m = (T + per - 1) / per;
-            double cost = (double)((units * m + 147) / 148) * (per + 1.5);
-            if (m > 1) cost += (double)((state_units * (m - 1) * q + 147) / 148) * (0.6 * per / q + 1.5) + 2 + 0.1 * m * q;
-            else if (q > 1) continue;
+            if (m < 2) continue;
+            const double cost = 1.08 * (phase(units * m, per, chunk, bytes) + phase(sets * state_units * (m - 1) * q, per / q, state_chunk, bytes / 2) + more + 0.06 * (m - 1) * q);
             if (cost < best) { best = cost; nseg = m; cps = per; sub = q; }
         }
     }
@@ -681,8 +702,8 @@ void decay_tc_split(darkattn_decay_plan_s *plan)
 {
     const darkattn_decay_desc_t &ds = plan->desc;
     const int T = (ds.N + C - 1) / C;
-    pick(T, (long long)ds.B * ds.H, (long long)ds.B * ds.H_kv, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub);
-    pick(T, 3LL * ds.B * ds.H, 2LL * ds.B * ds.H, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub);
+    pick(T, ds.d, ds.dv, (long long)ds.B * ds.H, (long long)ds.B * ds.H_kv, 1, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub);
+    pick(T, ds.d, ds.dv, 3LL * ds.B * ds.H, (long long)ds.B * ds.H, 2, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub);
 }
 
 darkattn_status_t decay_tc_run(DecayArgs &A, DecayPass *state_pass, int nstate, cudaStream_t st)
@@ -690,7 +711,7 @@ darkattn_status_t decay_tc_run(DecayArgs &A, DecayPass *state_pass, int nstate, 
     if (A.nseg > 1) {
         const DecayArgs P = decay_pieces(A, state_pass, nstate);
         if (darkattn_status_t rc = launch_all<false>(P, P.pass, nstate, true, st)) return rc;
-        for (int i = 0; i < nstate; ++i) DARKATTN_CUDA_TRY(decay_scan_pieces(P, state_pass[i], C, st), "decay_scan_kernel");
+        for (int i = 0; i < nstate; ++i) DARKATTN_CUDA_TRY(decay_scan_pieces(P, state_pass[i], C, true, st), "decay_scan_kernel");
     }
     return launch_all<true>(A, A.pass, A.npass, A.nseg == 1, st);
 }
