@@ -322,6 +322,7 @@ class DecayPlan:
         self._q, self._k = (ds.B, ds.H, ds.N, ds.d), (ds.B, ds.H_kv, ds.N, ds.d)
         self._v, self._o = (ds.B, ds.H_kv, ds.N, ds.dv), (ds.B, ds.H, ds.N, ds.dv)
         self._s = (ds.B, ds.H_kv, ds.d, ds.dv)
+        self._g, self._n, self._ws = (ds.H_kv,), (ds.B,), self.workspace_bytes
         self._token = [(ds.B, ds.H, ds.d), (ds.B, ds.H_kv, ds.d), (ds.B, ds.H_kv, ds.dv), (ds.B, ds.H, ds.dv)]
 
     @property
@@ -355,55 +356,74 @@ def darkattn_decay_plan(B, H, N, d, *, dv=0, dtype=BF16, H_kv=0, path=PATH_AUTO,
     return DecayPlan(h.value, desc)
 
 
-def _arg(t, name, shape, dtype, device=None):
+_F32, _I32 = torch.float32, torch.int32
+
+
+def _arg(t, name, shape, dtype, device):
     """A tensor's address, after the checks that keep the kernels inside of it."""
     if t is None:
         return None
+    if t.shape == shape and t.dtype is dtype and t.get_device() == device and t.is_contiguous():
+        return t.data_ptr()
     if t.shape != shape or t.dtype != dtype:
         raise ValueError(f"{name} is {t.dtype} {tuple(t.shape)}: {dtype} {tuple(shape)} is expected")
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} has to be a contiguous CUDA tensor")
-    if t.get_device() != (torch.cuda.current_device() if device is None else device):
-        raise ValueError(f"{name} is on another device than the current one")
-    return t.data_ptr()
+    raise ValueError(f"{name} is on another device than the current one")
+
+
+_get_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
+def _device():
+    """The current device, without the module's first-use checks once it is in use."""
+    return _get_device() if _get_device is not None and torch.cuda.is_initialized() else torch.cuda.current_device()
+
+
+def _stream_of(stream, device):
+    return _raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream)
 
 
 def _workspace(plan, t, device):
-    if t.numel() * t.element_size() < plan.workspace_bytes:
-        raise ValueError(f"workspace has {t.numel() * t.element_size()} bytes: {plan.workspace_bytes} are needed")
+    if t.numel() * t.element_size() < plan._ws:
+        raise ValueError(f"workspace has {t.numel() * t.element_size()} bytes: {plan._ws} are needed")
     return _arg(t, "workspace", t.shape, t.dtype, device)
 
 
 def darkattn_decay_forward(plan: DecayPlan, Q, K, V, log_decay, O, workspace, lengths=None, S_in=None, S_out=None, stream=None):
-    p, dt, dev = plan, plan._dt, torch.cuda.current_device()
+    p, dt, dev = plan, plan._dt, _device()
     _check(lib.darkattn_decay_forward(p.handle, _arg(Q, "Q", p._q, dt, dev), _arg(K, "K", p._k, dt, dev), _arg(V, "V", p._v, dt, dev),
-                                      _arg(log_decay, "log_decay", (p.desc.H_kv,), torch.float32, dev),
-                                      _arg(lengths, "lengths", (p.desc.B,), torch.int32, dev), _arg(S_in, "S_in", p._s, torch.float32, dev),
-                                      _arg(O, "O", p._o, dt, dev), _arg(S_out, "S_out", p._s, torch.float32, dev), _workspace(p, workspace, dev),
-                                      _stream(stream)), "darkattn_decay_forward")
+                                      _arg(log_decay, "log_decay", p._g, _F32, dev),
+                                      _arg(lengths, "lengths", p._n, _I32, dev), _arg(S_in, "S_in", p._s, _F32, dev),
+                                      _arg(O, "O", p._o, dt, dev), _arg(S_out, "S_out", p._s, _F32, dev), _workspace(p, workspace, dev),
+                                      _stream_of(stream, dev)), "darkattn_decay_forward")
     return O
 
 
 def darkattn_decay_backward(plan: DecayPlan, Q, K, V, log_decay, dO, dQ, dK, dV, workspace, lengths=None, S_in=None, dS_out=None, dS_in=None,
                             stream=None):
-    p, dt, dev = plan, plan._dt, torch.cuda.current_device()
+    p, dt, dev = plan, plan._dt, _device()
     _check(lib.darkattn_decay_backward(p.handle, _arg(Q, "Q", p._q, dt, dev), _arg(K, "K", p._k, dt, dev), _arg(V, "V", p._v, dt, dev),
-                                       _arg(log_decay, "log_decay", (p.desc.H_kv,), torch.float32, dev),
-                                       _arg(lengths, "lengths", (p.desc.B,), torch.int32, dev), _arg(S_in, "S_in", p._s, torch.float32, dev),
-                                       _arg(dO, "dO", p._o, dt, dev), _arg(dS_out, "dS_out", p._s, torch.float32, dev), _arg(dQ, "dQ", p._q, dt, dev),
-                                       _arg(dK, "dK", p._k, dt, dev), _arg(dV, "dV", p._v, dt, dev), _arg(dS_in, "dS_in", p._s, torch.float32, dev),
-                                       _workspace(p, workspace, dev), _stream(stream)), "darkattn_decay_backward")
+                                       _arg(log_decay, "log_decay", p._g, _F32, dev),
+                                       _arg(lengths, "lengths", p._n, _I32, dev), _arg(S_in, "S_in", p._s, _F32, dev),
+                                       _arg(dO, "dO", p._o, dt, dev), _arg(dS_out, "dS_out", p._s, _F32, dev), _arg(dQ, "dQ", p._q, dt, dev),
+                                       _arg(dK, "dK", p._k, dt, dev), _arg(dV, "dV", p._v, dt, dev), _arg(dS_in, "dS_in", p._s, _F32, dev),
+                                       _workspace(p, workspace, dev), _stream_of(stream, dev)), "darkattn_decay_backward")
     return dQ, dK, dV
 
 
 def darkattn_decay_step(plan: DecayPlan, q, k, v, log_decay, S, o, slots=None, stream=None):
     """One token of each sequence: the pool of states S [n_slots, H_kv, d, dv] is updated in place, o receives the output."""
-    p, dt, dev = plan, plan._dt, torch.cuda.current_device()
-    qs, ks, vs, os_ = p._token
-    _check(lib.darkattn_decay_step(p.handle, _arg(q, "q", qs, dt, dev), _arg(k, "k", ks, dt, dev), _arg(v, "v", vs, dt, dev),
-                                   _arg(log_decay, "log_decay", (p.desc.H_kv,), torch.float32, dev), _arg(S, "S", S.shape[:1] + p._s[1:], torch.float32, dev),
-                                   _arg(slots, "slots", (p.desc.B,), torch.int32, dev), S.shape[0], _arg(o, "o", os_, dt, dev), _stream(stream)),
-           "darkattn_decay_step")
+    # (one token's launch takes a few microseconds: the checks are laid out in a row)
+    dt, dev = plan._dt, _device()
+    qs, ks, vs, os_ = plan._token
+    pool = S.shape
+    rc = lib.darkattn_decay_step(plan.handle, _arg(q, "q", qs, dt, dev), _arg(k, "k", ks, dt, dev), _arg(v, "v", vs, dt, dev),
+                                 _arg(log_decay, "log_decay", plan._g, _F32, dev), _arg(S, "S", (pool[0],) + plan._s[1:] if pool else (), _F32, dev),
+                                 None if slots is None else _arg(slots, "slots", plan._n, _I32, dev), pool[0], _arg(o, "o", os_, dt, dev),
+                                 _stream_of(stream, dev))
+    if rc:
+        _check(rc, "darkattn_decay_step")
     return o
 
 
@@ -411,25 +431,32 @@ def darkattn_decay_last_device_status(plan: DecayPlan, workspace, stream=None) -
     return int(lib.darkattn_decay_last_device_status(plan.handle, _ptr(workspace), _stream(stream)))
 
 
-def _state_args(S, codes, scales, slots, format):
-    dev = torch.cuda.current_device()
-    if S.dim() < 2 or codes.dim() != S.dim() or codes.element_size() != 1:
+def _state_args(S, codes, scales, slots, dev):
+    """(B, rows, cols) and n_slots, after the checks; the addresses are the caller's to take."""
+    shape, kept = S.shape, codes.shape
+    if len(shape) < 2 or len(kept) != len(shape) or codes.element_size() != 1:
         raise ValueError("S is [B, ..., cols], codes one byte an element [n_slots, ..., cols]")
-    n, cols = codes.shape[0], S.shape[-1]
-    args = (_arg(S, "S", S.shape, torch.float32, dev), _arg(codes, "codes", (n,) + tuple(S.shape[1:]), codes.dtype, dev),
-            _arg(scales, "scales", (n,) + tuple(S.shape[1:-1]), torch.float32, dev), _arg(slots, "slots", S.shape[:1], torch.int32, dev))
-    B = S.shape[0]
-    return (B, S.numel() // max(B * cols, 1), cols, n, int(format)) + args
+    if kept[1:] != shape[1:]:
+        raise ValueError(f"codes is {tuple(kept)}: {(kept[0],) + tuple(shape[1:])} is expected")
+    B, cols = shape[0], shape[-1]
+    return (B, S.numel() // max(B * cols, 1), cols, kept[0], _arg(S, "S", shape, _F32, dev), _arg(codes, "codes", kept, codes.dtype, dev),
+            _arg(scales, "scales", kept[:-1], _F32, dev), None if slots is None else _arg(slots, "slots", shape[:1], _I32, dev))
 
 
 def darkattn_state_store(S, codes, scales, slots=None, format=STATE_I8, stream=None):
     """Rows of S [B, ..., cols] into the 8-bit cache codes [n_slots, ..., cols], scales [n_slots, ...]."""
-    B, rows, cols, n, fmt, S_, c_, sc_, sl_ = _state_args(S, codes, scales, slots, format)
-    _check(lib.darkattn_state_store(B, rows, cols, S_, sl_, n, fmt, c_, sc_, _stream(stream)), "darkattn_state_store")
+    dev = _device()
+    B, rows, cols, n, S_, c_, sc_, sl_ = _state_args(S, codes, scales, slots, dev)
+    rc = lib.darkattn_state_store(B, rows, cols, S_, sl_, n, format, c_, sc_, _stream_of(stream, dev))
+    if rc:
+        _check(rc, "darkattn_state_store")
 
 
 def darkattn_state_load(codes, scales, S, slots=None, format=STATE_I8, stream=None):
     """Rows of the 8-bit cache back into S [B, ..., cols]."""
-    B, rows, cols, n, fmt, S_, c_, sc_, sl_ = _state_args(S, codes, scales, slots, format)
-    _check(lib.darkattn_state_load(B, rows, cols, c_, sc_, sl_, n, fmt, S_, _stream(stream)), "darkattn_state_load")
+    dev = _device()
+    B, rows, cols, n, S_, c_, sc_, sl_ = _state_args(S, codes, scales, slots, dev)
+    rc = lib.darkattn_state_load(B, rows, cols, c_, sc_, sl_, n, format, S_, _stream_of(stream, dev))
+    if rc:
+        _check(rc, "darkattn_state_load")
     return S
