@@ -1,8 +1,8 @@
 // Attention with a decay per head in FP32 arithmetic: any width up to 512, any length, fp32 or bf16 in memory.
 //
-// A block takes a segment of one head's chunks in the pass's order (64 rows a chunk) and TZ columns of the output; the state's
-// columns stay in shared memory for the whole segment. Per chunk four products, 256 threads with 4 x 4 or 4 x 8 numbers each:
-// scores X Y^T, X S, the state's update Y^T Z, and P Z.
+// A block takes a segment of one head's chunks in the pass's order (64 rows a chunk), per chunk four products: scores X Y^T, X S, the
+// state's update Y^T Z, and P Z. Widths up to 128 have kernels of their own below; wider ones go by slices of 64 and tiles of TZ columns
+// of the output, whose share of the state stays in shared memory for the whole segment.
 #include "decay.cuh"
 
 #include <float.h>
@@ -179,6 +179,282 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
     }
 }
 
+// ---------------------------------------------------------------- widths up to 128
+// The whole width of X, Y and Z at once: 256 threads, thread (ty, tx) holds R x R numbers of the state in registers (rows of ty, columns of tx)
+// and 4 x R of the rows out. R = 4, 5, 6 or 8 for widths up to 64, 80, 96, 128. Products two numbers at a time (FFMA2: an FFMA was measured
+// at 2.3 cycles a scheduler, an FFMA2, twice the work, at 2.0).
+__device__ __forceinline__ int spot(int t, int v, int R) { return v < 4 ? t * 4 + v : 64 + t * (R - 4) + v - 4; }
+
+// The R numbers of thread t's spots, from a row
+template <int R>
+__device__ __forceinline__ void take(float (&y)[8], const float *row, int t)
+{
+    *reinterpret_cast<float4 *>(y) = *reinterpret_cast<const float4 *>(row + t * 4);
+    if (R == 5) y[4] = row[64 + t];
+    if (R == 6) *reinterpret_cast<float2 *>(y + 4) = *reinterpret_cast<const float2 *>(row + 64 + t * 2);
+    if (R == 8) *reinterpret_cast<float4 *>(y + 4) = *reinterpret_cast<const float4 *>(row + 64 + t * 4);
+}
+__device__ __forceinline__ unsigned long long pair(float a, float b)
+{
+    unsigned long long r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void fma_pair(unsigned long long &acc, unsigned long long a, unsigned long long b)
+{
+    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(a), "l"(b));
+}
+__device__ __forceinline__ float2 both(unsigned long long a)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+    return r;
+}
+// Numbers of one row by columns: pairs, and one alone where R is odd
+template <int R> struct Row {
+    unsigned long long p[R / 2];
+    float last;
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < R / 2; ++i) p[i] = 0ull;
+        last = 0.f;
+    }
+    __device__ __forceinline__ void scale(float f)
+    {
+        const unsigned long long f2 = pair(f, f);
+#pragma unroll
+        for (int i = 0; i < R / 2; ++i) asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(p[i]) : "l"(f2));
+        last *= f;
+    }
+    __device__ __forceinline__ void add(float x, const unsigned long long (&y)[4], float ylast)
+    {
+        const unsigned long long x2 = pair(x, x);
+#pragma unroll
+        for (int i = 0; i < R / 2; ++i) fma_pair(p[i], x2, y[i]);
+        if (R & 1) last = fmaf(x, ylast, last);
+    }
+    __device__ __forceinline__ float get(int v) const
+    {
+        if ((R & 1) && v == R - 1) return last;
+        const float2 b = both(p[v / 2]);
+        return v & 1 ? b.y : b.x;
+    }
+    // to thread t's spots of a row in shared memory
+    __device__ __forceinline__ void put(float *row, int t) const
+    {
+        *reinterpret_cast<float4 *>(row + t * 4) = make_float4(get(0), get(1), get(2), get(3));
+        if (R == 5) row[64 + t] = get(4);
+        if (R == 6) *reinterpret_cast<float2 *>(row + 64 + t * 2) = make_float2(get(4), get(5));
+        if (R == 8) *reinterpret_cast<float4 *>(row + 64 + t * 4) = make_float4(get(4), get(5), get(6), get(7));
+    }
+    __device__ __forceinline__ void set(int v, float x)
+    {
+        if ((R & 1) && v == R - 1) { last = x; return; }
+        const float2 b = both(p[v / 2]);
+        p[v / 2] = v & 1 ? pair(b.x, x) : pair(x, b.y);
+    }
+};
+// acc[u] += sum over k < K of a_u[k] b[k][columns of tx]: a_u[k] the u-th number of ty in row k of A (RA of them)
+template <int RA, int R, int RB>
+__device__ __forceinline__ void products(Row<R> (&acc)[RA], const float *A, int lda, const float *B, int ldb, int K, int ty, int tx)
+{
+#pragma unroll 4
+    for (int k = 0; k < K; ++k) {
+        float x[8], y[8];
+        take<RA>(x, A + k * lda, ty);
+        take<RB>(y, B + k * ldb, tx);
+        unsigned long long y2[4];
+#pragma unroll
+        for (int i = 0; i < R / 2; ++i) y2[i] = pair(y[2 * i], y[2 * i + 1]);
+#pragma unroll
+        for (int u = 0; u < RA; ++u) acc[u].add(x[u], y2, y[R - 1]);
+    }
+}
+
+template <int R>
+struct TileSmem {
+    static constexpr int LW = R == 4 ? 64 : 64 + 16 * (R - 4);                       // widest row
+    // P takes the place of Y transposed when the scores are there: so two blocks of 80 columns fit an SM
+    static constexpr int XT = 0, YT = XT + LW * kPad, PT = YT, Yw = YT + LW * kPad, Z = Yw + C * LW, S = Z + C * LW, pw = S + LW * LW, total = (pw + 72) * 4;
+    static_assert(total <= 232448, "shared memory of a block");
+};
+
+// four numbers of a row of `width`, zeros behind its end
+template <typename T>
+__device__ __forceinline__ float4 load4(const T *row, int f, int width, bool vec)
+{
+    float4 x = make_float4(0, 0, 0, 0);
+    if (vec) {
+        if (f < width) {
+            if constexpr (sizeof(T) == 4) x = *reinterpret_cast<const float4 *>(row + f);
+            else {
+                const uint2 r = *reinterpret_cast<const uint2 *>(row + f);
+                x = make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u), __uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u));
+            }
+        }
+        return x;
+    }
+    if (f < width) x.x = to_f(row[f]);
+    if (f + 1 < width) x.y = to_f(row[f + 1]);
+    if (f + 2 < width) x.z = to_f(row[f + 2]);
+    if (f + 3 < width) x.w = to_f(row[f + 3]);
+    return x;
+}
+
+__device__ __forceinline__ void store4(float *at, float a, float b, float c, float d) { *reinterpret_cast<float4 *>(at) = make_float4(a, b, c, d); }
+__device__ __forceinline__ void store4(__nv_bfloat16 *at, float a, float b, float c, float d)
+{
+    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b), y = __floats2bfloat162_rn(c, d);
+    *reinterpret_cast<uint2 *>(at) = make_uint2(*reinterpret_cast<const unsigned *>(&x), *reinterpret_cast<const unsigned *>(&y));
+}
+
+template <typename T, int R, bool MAIN>
+__global__ void __launch_bounds__(kThreadsS) decay_tile_kernel(const __grid_constant__ DecayArgs A)
+{
+    using M = TileSmem<R>;
+    constexpr int LW = M::LW;
+    extern __shared__ __align__(16) float sm[];
+    float *XT = sm + M::XT, *YT = sm + M::YT, *Yw = sm + M::Yw, *Zs = sm + M::Z, *PT = sm + M::PT, *Ss = sm + M::S, *pw = sm + M::pw;
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, warp = tid >> 5, lane = tid & 31;
+    pdl_wait();
+    if (MAIN && blockIdx.x == 0 && tid == 0) *A.status = 0;     // (nothing here waits: the call's status is known)
+
+    const int nseg = MAIN ? A.nseg : A.nseg - 1;
+    int id = blockIdx.x;
+    const DecayPass &p = A.pass[id % A.npass]; id /= A.npass;
+    const int seg = id % nseg, head = id / nseg, HX = MAIN ? p.HX : A.Hkv;
+    if (head >= A.B * HX) return;
+    const int b = head / HX, hx = head % HX, hs = hx / (HX / A.Hkv);
+    const int G = p.HY > HX ? p.HY / HX : 1, hy0 = p.HY > HX ? hx * G : hx / (HX / p.HY);
+    const DecaySpan sp = decay_span<C>(A, b, seg);
+    const int a = p.a, c = p.c, reverse = p.reverse;
+    const bool va = a % 4 == 0, vc = c % 4 == 0;
+    const bool last = sp.T == 0 ? seg == 0 : sp.k0 < sp.k1 && sp.k1 == sp.T;
+    const size_t state = (size_t)(b * A.Hkv + hs) * a * c;
+    float *S_out = MAIN ? (p.S_out && last && hx % (HX / A.Hkv) == 0 ? p.S_out + state : nullptr)
+                        : const_cast<float *>(p.seg) + ((size_t)(b * A.Hkv + hs) * nseg + seg) * a * c;
+    if (sp.k0 == sp.k1 && !(MAIN && last && S_out)) return;
+    if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
+    const float *S_in = nullptr;
+    if (MAIN) S_in = seg == 0 ? (p.S_in ? p.S_in + state : nullptr) : p.seg + ((size_t)(b * A.Hkv + hs) * (nseg - 1) * A.sub + seg * A.sub - 1) * a * c;
+
+    Row<R> s[R];                                             // rows spot(ty, u), columns spot(tx, v)
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+        s[u].clear();
+#pragma unroll
+        for (int v = 0; v < R; ++v) {
+            const int f = spot(ty, u, R), z = spot(tx, v, R);
+            if (S_in && f < a && z < c) s[u].set(v, p.trans ? S_in[(size_t)z * a + f] : S_in[(size_t)f * c + z]);
+        }
+    }
+    const auto put_state = [&]() {
+#pragma unroll
+        for (int u = 0; u < R; ++u) s[u].put(Ss + spot(ty, u, R) * LW, tx);
+    };
+    if (MAIN) put_state();
+    const T *X = static_cast<const T *>(p.X) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * a;
+    T *O = static_cast<T *>(p.O) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * c;
+
+    for (int k = sp.k0; k < sp.k1; ++k) {
+        const int t0 = (reverse ? sp.T - 1 - k : k) * C, L = min(C, sp.n - t0);
+        Row<R> o[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) o[u].clear();
+        for (int g = 0; g < G; ++g) {
+            const T *Y = static_cast<const T *>(p.Y) + ((size_t)(b * p.HY + hy0 + g) * A.N + t0) * a;
+            const T *Z = static_cast<const T *>(p.Z) + ((size_t)(b * p.HY + hy0 + g) * A.N + t0) * c;
+            __syncthreads();                                 // the tiles of the step before have been read; pw and the state are there
+            // a warp brings 8 rows by 16 columns at a time: whole sectors, and two-way bank conflicts where it stores them transposed
+#pragma unroll 2
+            for (int i = warp; i < LW / 16 * 8; i += 8) {
+                const int r = (i & 7) * 8 + (lane >> 2), f = (i >> 3) * 16 + (lane & 3) * 4;
+                float4 y = make_float4(0, 0, 0, 0), z = y, x = y;
+                if (r < L) {
+                    y = load4(Y + (size_t)r * a, f, a, va);
+                    z = load4(Z + (size_t)r * c, f, c, vc);
+                    if (MAIN && g == 0) x = load4(X + (size_t)(t0 + r) * a, f, a, va);
+                }
+                *reinterpret_cast<float4 *>(Zs + r * LW + f) = z;
+                if (MAIN) {
+                    YT[f * kPad + r] = y.x; YT[(f + 1) * kPad + r] = y.y; YT[(f + 2) * kPad + r] = y.z; YT[(f + 3) * kPad + r] = y.w;
+                    if (g == 0) { XT[f * kPad + r] = x.x; XT[(f + 1) * kPad + r] = x.y; XT[(f + 2) * kPad + r] = x.z; XT[(f + 3) * kPad + r] = x.w; }
+                }
+                const float w = r < L ? pw[reverse ? r + 1 : L - 1 - r] * p.tok_mul : 0.f;
+                *reinterpret_cast<float4 *>(Yw + r * LW + f) = make_float4(y.x * w, y.y * w, y.z * w, y.w * w);
+            }
+            __syncthreads();
+            if (MAIN) {
+                Row<4> sc[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) sc[u].clear();
+                products<4, 4, 4>(sc, XT, kPad, YT, kPad, a, ty, tx);
+                if (g == 0) {
+                    products<4, R, R>(o, XT, kPad, Ss, LW, a, ty, tx);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const int r = ty * 4 + u;
+                        o[u].scale(r < L ? pw[reverse ? L - 1 - r : r + 1] * p.row_mul : 0.f);
+                    }
+                }
+                __syncthreads();                             // Y transposed has been read
+                const int n0 = reverse ? tx * 4 - ty * 4 : ty * 4 - tx * 4;      // distance of the 4 x 4 numbers' first
+                float w[7];                                  // decays of distances n0 - 3 .. n0 + 3
+#pragma unroll
+                for (int i = 0; i < 7; ++i) w[i] = n0 + i - 3 >= 0 ? pw[n0 + i - 3] * p.p_mul : 0.f;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    float x[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) x[u] = n0 + (reverse ? v - u : u - v) >= 0 ? sc[u].get(v) * (reverse ? w[3 + v - u] : w[3 + u - v]) : 0.f;
+                    *reinterpret_cast<float4 *>(PT + (tx * 4 + v) * kPad + ty * 4) = make_float4(x[0], x[1], x[2], x[3]);
+                }
+            }
+            if (k + 1 < sp.k1 || S_out) {                    // somebody reads the state behind this chunk
+                if (g == 0) {
+                    const float keep = pw[L];
+#pragma unroll
+                    for (int u = 0; u < R; ++u) s[u].scale(keep);
+                }
+                products<R, R, R>(s, Yw, LW, Zs, LW, L, ty, tx);
+            }
+            if (!MAIN) continue;
+            __syncthreads();                                 // P is there; the state before this chunk has been read
+            // rows 8 warp .. 8 warp + 7 of P: zero behind (backwards: before) the diagonal
+            const int from = reverse ? warp * 8 : 0, to = reverse ? L : min(warp * 8 + 8, L);
+            products<4, R, R>(o, PT + from * kPad, kPad, Zs + from * LW, LW, to - from, ty, tx);
+            if (g == G - 1) put_state();
+        }
+        if (MAIN) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int r = ty * 4 + u;
+                if (r >= L) continue;
+                T *at = O + (size_t)(t0 + r) * c;
+                if (vc) {
+                    if (tx * 4 < c) store4(at + tx * 4, o[u].get(0), o[u].get(1), o[u].get(2), o[u].get(3));
+                    if (R == 8 && 64 + tx * 4 < c) store4(at + 64 + tx * 4, o[u].get(4), o[u].get(5), o[u].get(6), o[u].get(7));
+                }
+#pragma unroll
+                for (int v = 0; v < R; ++v) {
+                    const int z = spot(tx, v, R);
+                    if (z < c && !(vc && (v < 4 || R == 8))) at[z] = from_f<T>(o[u].get(v));
+                }
+            }
+        }
+    }
+    if (S_out) {
+#pragma unroll
+        for (int u = 0; u < R; ++u)
+#pragma unroll
+            for (int v = 0; v < R; ++v) {
+                const int f = spot(ty, u, R), z = spot(tx, v, R);
+                if (f < a && z < c) S_out[(size_t)f * c + z] = s[u].get(v);
+            }
+    }
+}
+
 // One thread per element of the state, along the segments. Tokens of segment s: whole chunks, but for a pass backwards, whose first
 // chunk may be a short one.
 __global__ void __launch_bounds__(256) decay_scan_kernel(const __grid_constant__ DecayArgs A, const __grid_constant__ DecayPass p, int chunk, int by4)
@@ -211,6 +487,20 @@ __global__ void __launch_bounds__(256) decay_scan_kernel(const __grid_constant__
     }
 }
 
+template <typename T, int R, bool MAIN>
+cudaError_t launch_tile(const DecayArgs &A, cudaStream_t st)
+{
+    int heads = 0;
+    for (int i = 0; i < A.npass; ++i) heads = max(heads, MAIN ? A.B * A.pass[i].HX : A.B * A.Hkv);
+    const long long blocks = (long long)A.npass * (MAIN ? A.nseg : A.nseg - 1) * heads;
+    // Few blocks by an ordinary launch: such as start early, while the kernel before is still on some of the SMs, go two to an SM on the others
+    // (24 heads of 1000 tokens, d 80, in four segments: 127 us, by an ordinary launch 90; in 16 segments 63.5 and 66).
+    if (blocks > 148) return launch_pdl(decay_tile_kernel<T, R, MAIN>, dim3((unsigned)blocks), dim3(kThreadsS), TileSmem<R>::total, st, A);
+    if (cudaError_t e = allow_smem(reinterpret_cast<const void *>(decay_tile_kernel<T, R, MAIN>), TileSmem<R>::total)) return e;
+    decay_tile_kernel<T, R, MAIN><<<dim3((unsigned)blocks), dim3(kThreadsS), TileSmem<R>::total, st>>>(A);
+    return cudaGetLastError();
+}
+
 template <typename T, int TZ, bool MAIN>
 cudaError_t launch(const DecayArgs &A, cudaStream_t st)
 {
@@ -229,7 +519,9 @@ cudaError_t launch_t(const DecayArgs &A, cudaStream_t st)
 {
     int a = 0, c = 0;
     for (int i = 0; i < A.npass; ++i) { a = max(a, A.pass[i].a); c = max(c, A.pass[i].c); }
-    return a <= 128 && c > 64 ? launch<T, 128, MAIN>(A, st) : launch<T, 64, MAIN>(A, st);
+    const int w = max(a, c);
+    return w <= 64 ? launch_tile<T, 4, MAIN>(A, st) : w <= 80 ? launch_tile<T, 5, MAIN>(A, st) : w <= 96 ? launch_tile<T, 6, MAIN>(A, st)
+           : w <= 128 ? launch_tile<T, 8, MAIN>(A, st) : launch<T, 64, MAIN>(A, st);
 }
 
 }  // namespace
@@ -264,16 +556,20 @@ darkattn_status_t decay_simt_run(DecayArgs &A, DecayPass *state_pass, int nstate
     return DARKATTN_OK;
 }
 
-// Segments: as many as shorten the longest chain of chunks by more than the states' own pass and the sum over them cost. In units of a
-// chunk's time; a chunk of the states' pass is one product of four.
-static void pick(int T, long long units, long long state_units, int slots, int &nseg, int &cps, int &sub)
+// Segments: the cheapest by an estimate in units of a chunk's time (fitted to fp32 on a B200: 11 us at width 64 and 22 at 128 by itself, two blocks
+// on an SM 1.35 times that): a chunk of the states alone takes 0.28, three kernels instead of one about one more.
+static void pick(int T, long long units, long long state_units, int per_sm, int &nseg, int &cps, int &sub)
 {
-    double best = 1e30;
-    sub = 1;
-    for (int n = 1; n <= T && n <= 128; ++n) {
+    const auto phase = [&](long long blocks, int per, double one) {
+        const double two = per_sm == 2 ? 1.35 : 1.0;
+        const long long slots = 148LL * per_sm, rest = blocks % slots;
+        return per * one * ((double)(blocks / slots) * two + (rest > 148 ? two : rest ? 1.0 : 0.0));
+    };
+    nseg = 1; cps = T; sub = 1;
+    double best = phase(units, T, 1.0);
+    for (int n = 2; n <= T && n <= 128; ++n) {
         const int per = (T + n - 1) / n, m = (T + per - 1) / per;
-        double cost = (double)((units * m + slots - 1) / slots) * (per + 1);
-        if (m > 1) cost += (double)((state_units * (m - 1) + slots - 1) / slots) * (0.5 * per + 1) + 2 + 0.1 * m;
+        const double cost = phase(units * m, per, 1.0) + phase(state_units * (m - 1), per, 0.28) + 1.0 + 0.01 * m;
         if (cost < best) { best = cost; nseg = m; cps = per; }
     }
 }
@@ -282,11 +578,13 @@ void decay_simt_split(darkattn_decay_plan_s *plan)
 {
     const darkattn_decay_desc_t &ds = plan->desc;
     const int T = (ds.N + C - 1) / C, w = ds.d > ds.dv ? ds.d : ds.dv;
-    const int tz = w <= 128 && w > 64 ? 128 : 64;
-    const long long zf = (ds.dv + tz - 1) / tz, zb = (w + tz - 1) / tz;
-    const int slots = w <= 64 ? 296 : 148;
-    pick(T, (long long)ds.B * ds.H * zf, (long long)ds.B * ds.H_kv * zf, slots, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub);
-    pick(T, (long long)ds.B * (ds.H + 2 * ds.H) * zb, 2LL * ds.B * ds.H * zf, slots, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub);
+    const long long zf = w <= 128 ? 1 : (ds.dv + 63) / 64, zb = w <= 128 ? 1 : (w + 63) / 64;      // tiles of the output's columns
+    const int per_sm = w <= 80 ? 2 : 1;
+    pick(T, (long long)ds.B * ds.H * zf, (long long)ds.B * ds.H_kv * zf, per_sm, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub);
+    pick(T, (long long)ds.B * (ds.H + 2 * ds.H) * zb, 2LL * ds.B * ds.H * zf, per_sm, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub);
+#ifdef FORCE
+    if (getenv("NSEG")) { int n = atoi(getenv("NSEG")), q = atoi(getenv("SUB")); for (int i = 0; i < 2; ++i) { auto &f = i ? plan->bwd : plan->fwd; f.cps = ((T + n - 1) / n + q - 1) / q * q; f.nseg = (T + f.cps - 1) / f.cps; f.sub = q; } }
+#endif
 }
 
 }  // namespace darkattn

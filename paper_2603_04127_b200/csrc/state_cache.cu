@@ -85,7 +85,7 @@ __device__ __forceinline__ bool taken_before(const int *slots, int b, int slot)
 }
 
 // V: vectors of four a lane holds of each row; L: lanes of a row (cols <= 4 L V, a multiple of four: with all 32 on rows of 64 numbers half of them
-// had nothing to do, 12.4 us for what now takes XX). V = 0: any cols, the row read twice
+// had nothing to do, 12.4 us for what now takes 8.7). V = 0: any cols, the row read twice
 template <bool E4M3, int V, int L>
 __global__ void __launch_bounds__(kWarps * 32) state_store_kernel(const float *__restrict__ S, const int *__restrict__ slots, int n_slots, int rows, int cols,
                                                                   unsigned char *codes, float *scales)
