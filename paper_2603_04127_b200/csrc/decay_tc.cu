@@ -240,6 +240,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         if (p.S_out && last_seg && hx % (HX / A.Hkv) == 0) S_out = p.S_out + state;
     } else if (nchunk) S_out = const_cast<float *>(p.seg) + ((size_t)(b * A.Hkv + hs) * nseg + seg) * a * c;
     const bool has0 = MAIN && S_in != nullptr;
+    const int kept = MAIN && !S_out ? nchunk - 1 : nchunk;      // chunks behind which somebody reads the state
     const bool whole = MAIN ? S_out != nullptr : p.whole;   // three parts
     const auto first_row = [&](int k) { return (reverse ? sp.T - 1 - (sp.k0 + k) : sp.k0 + k) * C; };
     const auto load = [&](int it, int k, int g) {         // item `it`: chunk k, head g of those summed over
@@ -334,10 +335,12 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     }
                 }
             }
-            ok = wait_tries(bar + 8 * T_READY, it & 1, status);
-            if (!ok) break;
-            tc_fence_after();
-            if (elect_one()) {
+            if (k < kept) {
+                ok = wait_tries(bar + 8 * T_READY, it & 1, status);
+                if (!ok) break;
+                tc_fence_after();
+            }
+            if (k < kept && elect_one()) {
                 const uint64_t halves = make_sdesc(smem_u32(stage + M::kX + M::kY), 64 * 128, 1024);      // Z's rows 0 .. 63 and 64 .. 127 as columns side by side
                 for (int part = 0; part < parts; ++part) {
                     const uint32_t left = tmem + (part < 2 ? kB + kPart * part : kThird);
@@ -399,7 +402,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         int Ltok = -1;
         uint32_t inters = 0;
         // Brings item `it`'s weighted Y (of a chunk of L rows) into tensor memory.
-        const auto prepare = [&](int it, int L) {
+        const auto prepare = [&](int it, int k, int L) {
             const uint32_t stage = sbase + (it & 1) * M::kStage;
             DWAIT(FULL0 + (it & 1), (it >> 1) & 1);
             if (L != Ltok || L < C) {
@@ -425,6 +428,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 if (L < C) arrive_warp(bar + 8 * CLEAN, lane);
                 Ltok = L;
             }
+            if (k >= kept) return;
             if (rows_y) {
 #pragma unroll
                 for (int tb = 0; tb < (kHalves ? 2 : 4) / kGroups; ++tb) {
@@ -451,7 +455,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         }
         float x_row = 0.f;                                // of X S
         int Lx = -1;
-        if (items > 0) prepare(0, rows_of(0));
+        if (items > 0) prepare(0, 0, rows_of(0));
         for (int it = 0, k = 0, g = 0; it < items; ++it) {
             const int t0 = first_row(k), L = min(C, sp.n - t0);
             if (MAIN) {                                   // P: the lower (backwards: the upper) triangle, times the decays
@@ -524,8 +528,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 tc_fence_before();
                 arrive_warp(bar + 8 * P_READY, lane);
             }
-            DWAIT(DS, it & 1);
-            if (g == G - 1) {
+            if (k < kept) DWAIT(DS, it & 1);
+            if (k < kept && g == G - 1) {
                 tc_fence_after();
                 const float keep = pw[L];
                 constexpr int kLd = W < 32 ? W : 32;
@@ -575,7 +579,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 }
             }
             if (++g == G) { g = 0; ++k; }
-            if (it + 1 < items) prepare(it + 1, rows_of(k));
+            if (it + 1 < items) prepare(it + 1, k, rows_of(k));
         }
 #undef DWAIT
         if (!ok) *abort_flag = 1;
