@@ -242,7 +242,12 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     const bool has0 = MAIN && S_in != nullptr;
     const int kept = MAIN && !S_out ? nchunk - 1 : nchunk;      // chunks behind which somebody reads the state
     const bool whole = MAIN ? S_out != nullptr : p.whole;   // three parts
-    const auto first_row = [&](int k) { return (reverse ? sp.T - 1 - (sp.k0 + k) : sp.k0 + k) * C; };
+    // The states alone are summed from a piece's last chunk to its first (by the power of the decay to the piece's end): the pass that follows starts
+    // where this one ends, on what is then in L2.
+    const auto first_row = [&](int k) {
+        const int at = sp.k0 + (MAIN ? k : nchunk - 1 - k);
+        return (reverse ? sp.T - 1 - at : at) * C;
+    };
     const auto load = [&](int it, int k, int g) {         // item `it`: chunk k, head g of those summed over
         if (elect_one()) {
             const TcMaps &m = P.m[ip];
@@ -454,6 +459,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             p_row[i] = (reverse ? blk > quarter : blk < quarter) ? pw[reverse ? blk * 32 - row : row - blk * 32 - 31] : 1.f;
         }
         float x_row = 0.f;                                // of X S
+        float behind = 1.f;                               // (states alone) the decay from the chunk's end to the piece's
         int Lx = -1;
         if (items > 0) prepare(0, 0, rows_of(0));
         for (int it = 0, k = 0, g = 0; it < items; ++it) {
@@ -531,7 +537,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             if (k < kept) DWAIT(DS, it & 1);
             if (k < kept && g == G - 1) {
                 tc_fence_after();
-                const float keep = pw[L];
+                const float keep = MAIN ? pw[L] : 1.f, share = behind;
+                if (!MAIN) behind *= pw[L];
                 constexpr int kLd = W < 32 ? W : 32;
 #pragma unroll
                 for (int h = 0; h < W; h += kLd) {
@@ -539,7 +546,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     tmem_ld<kLd>(at + kD + half * 64 + z0 + h, o);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int j = 0; j < kLd; ++j) s[h + j] = fmaf(keep, s[h + j], f(o[j]));
+                    for (int j = 0; j < kLd; ++j) s[h + j] = MAIN ? fmaf(keep, s[h + j], f(o[j])) : fmaf(share, f(o[j]), s[h + j]);
                 }
                 if (MAIN) put_state();
                 tc_fence_before();
