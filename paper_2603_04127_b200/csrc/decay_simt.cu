@@ -582,9 +582,6 @@ void decay_simt_split(darkattn_decay_plan_s *plan)
     const int per_sm = w <= 80 ? 2 : 1;
     pick(T, (long long)ds.B * ds.H * zf, (long long)ds.B * ds.H_kv * zf, per_sm, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub);
     pick(T, (long long)ds.B * (ds.H + 2 * ds.H) * zb, 2LL * ds.B * ds.H * zf, per_sm, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub);
-#ifdef FORCE
-    if (getenv("NSEG")) { int n = atoi(getenv("NSEG")), q = atoi(getenv("SUB")); for (int i = 0; i < 2; ++i) { auto &f = i ? plan->bwd : plan->fwd; f.cps = ((T + n - 1) / n + q - 1) / q * q; f.nseg = (T + f.cps - 1) / f.cps; f.sub = q; } }
-#endif
 }
 
 }  // namespace darkattn

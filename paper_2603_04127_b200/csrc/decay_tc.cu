@@ -2,13 +2,19 @@
 //
 // One block takes a segment of one head's chunks in the pass's order; a chunk is four products of tcgen05.mma:
 //   A = X Y^T                        scores; times the decays and rounded to bf16 they go back to tensor memory as P, the left operand of
-//   O = lambda^(..) (X S) + P Z      the rows out: X S first, its rows scaled in place, P Z accumulated onto it
-//   D = (w Y)^T Z                    what the chunk adds to the state. The tokens' weights are applied in fp32 to Y as it goes, transposed,
-//                                    from shared memory into tensor memory, as two bf16 parts (16 bits and their signs), or three (24)
-//                                    where the caller gets the state: with one, the rounding would show in the rows out.
-// The state itself stays in the registers of 16 warps in fp32, S <- lambda^L S + D; the rows read a copy rounded to bf16 (as P is
-// rounded: half a step of each term, like the rounding of the rows out).
-// Everything moves by TMA, two chunks of X, Y and Z deep; the rows out are staged in the chunk's own tiles.
+//   O = lambda^(..) (X S) + P Z      the rows out: X S first, its rows scaled in place, P Z accumulated onto it (of narrow tiles apart)
+//   D = (w Y)^T Z                    what the chunk adds to the state. The tokens' weights are applied to Y as it goes, transposed, from shared
+//                                    memory into tensor memory, as two bf16 parts (16 bits), or three (24) where the caller gets the
+//                                    state; with one, its rounding would show in the rows out.
+// The state itself stays in the registers of eight warps in fp32, S <- lambda^L S + D; the rows read a copy rounded to bf16 (as P is
+// rounded: half a step of each term, like the rounding of the rows out: together 1.4 times the error of that rounding alone).
+// Everything moves by TMA, two chunks of X, Y and Z deep; the rows out are staged in the chunk's own tiles (stored from registers, 32 bytes a
+// thread, d 128 took 226 us for 212).
+//
+// What bounds it: shared memory. At width 128 a chunk's tiles, operands and copies are 3.8 thousand cycles of its 128 bytes a cycle (the products
+// by themselves 2.6), a chunk takes 4.5 thousand; at 64 2.3 of 3.4 thousand, the rest latencies of steps that wait for one another: scores
+// into P 500, the state 250 to 600, rows out 400, transposition 1100. (Warps of their own for some of the steps, 18 to 28 in all, overlap
+// them and made nothing faster: d 128 219 -> 275 us.) 4 x 37 heads of 8192 tokens, one block an SM: d 128 1.24 GB in 212 us, 5.9 TB/s; d 64 0.62 GB in 130, 4.8.
 #include "decay.cuh"
 #include "tc_common.cuh"
 
@@ -17,13 +23,9 @@ namespace {
 using namespace tc;
 
 constexpr int C = 128;
-// Column groups: kGroups warps share a quarter of the rows, each takes DZ / kGroups columns of O, D and the state. Beside them one warp
-// loads and stores, one issues products.
-#ifndef NCOLS
-#define NCOLS 2
-#endif
-constexpr int kGroups = NCOLS, kWarps = 4 * kGroups, kBlock = 32 * (kWarps + 2);
-static_assert(kGroups == 2 || kGroups == 4, "blocks of scores are shared out for these");
+// Two warps share a quarter of the rows, each takes half of the columns of O, D and the state (four with a quarter each: twice the waits and arrivals,
+// d 128 226 us for 220). Beside them one warp loads and stores, one issues products.
+constexpr int kGroups = 2, kWarps = 4 * kGroups, kBlock = 32 * (kWarps + 2);
 constexpr uint32_t kA = 0, kB = 128, kO = 256, kD = 384; // columns of tensor memory
 constexpr uint32_t kX = 320;                             // X S of a narrow Z (64 columns), apart from P Z; of a wide one it goes to kO
 constexpr int kDiag = 68;                                // numbers of each copy of the diagonal blocks' decays
@@ -42,12 +44,12 @@ struct TcSmem {
 };
 
 // tiles of 64 columns and 128 rows of one head: [heads, N, width]
-__device__ __forceinline__ void load3(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y, int z)
+__device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, uint64_t *bar, int x, int y, int z)
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z) : "memory");
 }
-__device__ __forceinline__ void store3(const CUtensorMap *map, const void *src, int x, int y, int z)
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, const void *src, int x, int y, int z)
 {
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z) : "memory");
@@ -57,21 +59,16 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t a, uint32_t (&
     if constexpr (N == 32) tmem_ld32(a, v);
     else tmem_ld16(a, v);
 }
-template <int N> __device__ __forceinline__ void tmem_st(uint32_t a, const uint32_t (&v)[N])
-{
-    if constexpr (N == 32) tmem_st32(a, v);
-    else tmem_st16(a, v);
-}
 __device__ __forceinline__ float f(uint32_t x) { return __uint_as_float(x); }
 
 // Shared memory by its 32-bit addresses: all of a block's are one number, read once, and constants.
-// A wait with a limit on the number of tries; one answer for the warp. The timer and the flag of tc::warp_wait cost a block of 64-column
-// tiles a tenth of its time. A try that finds nothing suspends the warp for a while, so that a healthy wait takes a few of them.
+// A wait with a limit on the number of tries; one answer for the warp. A try that finds nothing suspends the warp until the barrier's phase ends, 4 us
+// at most (measured), so that half a million are the 2 s of tc::warp_wait, whose timer and flag cost a block of 64-column tiles a tenth of its time.
 __device__ __forceinline__ bool wait_tries(uint32_t bar, uint32_t parity, int *status)
 {
     uint32_t ok;
     asm volatile(
-        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 2097152;\n\t"
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 500000;\n\t"
         "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
         "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n\t"
         "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
@@ -255,9 +252,9 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             const int t0 = first_row(k), hy = hy0 + g;
             uint64_t *full = bars + FULL0 + (it & 1);
             mbar_expect_tx(full, M::kStage);
-            if (MAIN) for (int x = 0; x < DY; x += 64) load3(stage + x * 256, &m.x, full, x, t0, head);
-            for (int x = 0; x < DY; x += 64) load3(stage + M::kX + x * 256, &m.y, full, x, t0, hy);
-            for (int x = 0; x < DZ; x += 64) load3(stage + M::kX + M::kY + x * 256, &m.z, full, x, t0, hy);
+            if (MAIN) for (int x = 0; x < DY; x += 64) tma_load_3d(stage + x * 256, &m.x, full, x, t0, head);
+            for (int x = 0; x < DY; x += 64) tma_load_3d(stage + M::kX + x * 256, &m.y, full, x, t0, hy);
+            for (int x = 0; x < DZ; x += 64) tma_load_3d(stage + M::kX + M::kY + x * 256, &m.z, full, x, t0, hy);
         }
     };
     const bool fine = *abort_flag == 0;
@@ -289,7 +286,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 if (MAIN && g2 == G - 1) {
                     ok = wait_tries(bar + 8 * STAGED, k2 & 1, status);
                     if (ok && sp.n - first_row(k2) >= C && elect_one()) {
-                        for (int x = 0; x < DZ && x < c; x += 64) store3(&m.o, stage + x * 256, x, first_row(k2), head);
+                        for (int x = 0; x < DZ && x < c; x += 64) tma_store_3d(&m.o, stage + x * 256, x, first_row(k2), head);
                         tma_store_commit();
                         tma_store_wait_read();
                     }
@@ -449,9 +446,9 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             arrive_warp(bar + 8 * T_READY, lane);
         };
         const auto rows_of = [&](int k) { return min(C, sp.n - first_row(k)); };
-        // Blocks of 32 columns of the scores: one a warp of four, the outer or the inner two a warp of two (the triangle has as much in either).
+        // Blocks of 32 columns of the scores: a warp takes the outer or the inner two (the triangle has as much in either).
         // Off the diagonal by column, and a power for the row, up to the block's near edge; on the diagonal by a table alone.
-        const auto block_of = [&](int i) { return kGroups == 4 ? cb : cb == 0 ? 3 * i : 1 + i; };
+        const auto block_of = [&](int i) { return cb == 0 ? 3 * i : 1 + i; };
         float p_row[4 / kGroups];
 #pragma unroll
         for (int i = 0; i < 4 / kGroups; ++i) {
@@ -474,24 +471,19 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     const bool off = reverse ? blk > quarter : blk < quarter;
                     if (off || blk == quarter) {
                         const float *by = off ? near : diag + (lane & 3) * kDiag + 32 - (lane & ~3);
-                        constexpr int kLd = DZ == 64 || kGroups == 2 ? 32 : 16;      // (registers)
+                        uint32_t v[32];
+                        tmem_ld32(at + kA + blk * 32, v);
+                        tmem_wait_ld();
 #pragma unroll
-                        for (int h = 0; h < 32; h += kLd) {
-                            uint32_t v[kLd];
-                            if constexpr (kLd == 32) tmem_ld32(at + kA + blk * 32, v);
-                            else tmem_ld16(at + kA + blk * 32 + h, v);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int j = 0; j < kLd; j += 4) {
-                                const float4 w = *reinterpret_cast<const float4 *>(by + h + j);
-                                float x[4] = {f(v[j]), f(v[j + 1]), f(v[j + 2]), f(v[j + 3])};
-                                mul2(x[0], x[1], p_row[i], p_row[i]);
-                                mul2(x[2], x[3], p_row[i], p_row[i]);
-                                mul2(x[0], x[1], w.x, w.y);
-                                mul2(x[2], x[3], w.z, w.w);
-                                pk[i][(h + j) / 2] = pack_bf16(x[0], x[1]);
-                                pk[i][(h + j) / 2 + 1] = pack_bf16(x[2], x[3]);
-                            }
+                        for (int j = 0; j < 32; j += 4) {
+                            const float4 w = *reinterpret_cast<const float4 *>(by + j);
+                            float x[4] = {f(v[j]), f(v[j + 1]), f(v[j + 2]), f(v[j + 3])};
+                            mul2(x[0], x[1], p_row[i], p_row[i]);
+                            mul2(x[2], x[3], p_row[i], p_row[i]);
+                            mul2(x[0], x[1], w.x, w.y);
+                            mul2(x[2], x[3], w.z, w.w);
+                            pk[i][j / 2] = pack_bf16(x[0], x[1]);
+                            pk[i][j / 2 + 1] = pack_bf16(x[2], x[3]);
                         }
                     } else {
 #pragma unroll
@@ -681,18 +673,18 @@ bool decay_tc_supported(const darkattn_decay_desc_t &ds)
 
 // Segments, and the pieces whose states are summed first: the cheapest by an estimate in us, fitted to measurements on a B200. A chunk takes 2.6 us
 // (wide tiles, 64 to 128 columns) or 1.7 us while few blocks run, and what the memory gives when all SMs do (5.7 and, power-bound, 4.8 TB/s);
-// a chunk of the states alone 1.4 or 1.0 us; two kernels more 13 or 6 us, twice that where there are two sets of states. One head of 8192 tokens, d 128: 178 us in one
+// a chunk of the states alone 1.4 or 1.0 us, a wave of blocks 2 us more; two kernels more 9 or 4 us, twice that where there are two sets of states. One head of 8192 tokens, d 128: 178 us in one
 // segment, 31 in 32; 4 x 16 heads: 164 in one, 139 in two with two pieces each, 188 in four; 8 heads of 65536, d 64: 113 in 18.
 // Segments have to promise 8 % (a backward pass in one segment shares more of its reads in L2 than the estimate knows: 4 x 16 heads, 337 us
 // in one, 359 in two).
 static void pick(int T, int d, int dv, long long units, long long state_units, int sets, int &nseg, int &cps, int &sub)
 {
     const bool wide = d > 64 || dv > 64;
-    const double chunk = wide ? 2.6 : 1.7, state_chunk = wide ? 1.4 : 1.0, more = sets * (wide ? 13 : 6), rate = wide ? 5.7e6 : 4.8e6;
+    const double chunk = wide ? 2.6 : 1.7, state_chunk = wide ? 1.4 : 1.0, more = sets * (wide ? 9 : 4), rate = wide ? 5.7e6 : 4.8e6;
     const double bytes = 2.0 * C * 2 * (d + dv);
     const auto phase = [&](long long blocks, int per, double us, double b) {
         const double all = 148 * b / rate, rest = (double)(blocks % 148) * b / rate;
-        return per * ((double)(blocks / 148) * (all > us ? all : us) + (blocks % 148 ? (rest > us ? rest : us) : 0));
+        return 2.0 * ((blocks + 147) / 148) + per * ((double)(blocks / 148) * (all > us ? all : us) + (blocks % 148 ? (rest > us ? rest : us) : 0));
     };
     nseg = 1; cps = T; sub = 1;
     double best = phase(units, T, chunk, bytes);
@@ -704,9 +696,6 @@ static void pick(int T, int d, int dv, long long units, long long state_units, i
             if (cost < best) { best = cost; nseg = m; cps = per; sub = q; }
         }
     }
-#ifdef FORCE
-    if (getenv("NSEG")) { int n = atoi(getenv("NSEG")), q = atoi(getenv("SUB")); cps = ((T + n - 1) / n + q - 1) / q * q; nseg = (T + cps - 1) / cps; sub = q; }
-#endif
 }
 
 void decay_tc_split(darkattn_decay_plan_s *plan)

@@ -273,6 +273,7 @@ def test_the_gradients_are_the_oracles_differences():
 SHAPES = [                                     # B, H, N, d, dv, H_kv
     (1, 1, 1, 8, 8, 1), (2, 2, 2, 5, 3, 2), (1, 2, 63, 16, 72, 1), (1, 3, 64, 65, 64, 3), (2, 4, 65, 64, 64, 2), (1, 2, 127, 128, 128, 2),
     (1, 2, 128, 64, 128, 1), (2, 1, 129, 128, 64, 1), (1, 6, 257, 80, 96, 3), (2, 2, 700, 40, 8, 2), (1, 1, 1500, 64, 64, 1), (1, 2, 300, 200, 130, 1),
+    (1, 16, 300, 64, 64, 1), (2, 8, 150, 128, 128, 1), (1, 2, 150, 97, 33, 1), (1, 1, 90, 100, 92, 1), (3, 1, 1100, 72, 128, 1), (1, 2, 640, 512, 24, 2),
 ]
 
 
@@ -604,6 +605,72 @@ def test_captured_calls_on_a_side_stream(binding, dtype):
         torch.cuda.synchronize()
         for k in eager:
             assert torch.equal(eager[k], a[k]) and torch.equal(a[k], b[k]), k
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_two_calls_at_once(binding, dtype):
+    """Two streams, a plan and a workspace each (and one plan for both): what each does by itself."""
+    kind = binding.BF16 if dtype == "bf16" else binding.F32
+    plan = binding.darkattn_decay_plan(2, 4, 3000, 64, dtype=kind)
+    sets = [dev(make(2, 4, 3000, 64, dtype=dtype, seed=60 + i)) for i in range(2)]
+    alone = []
+    for x in sets:
+        O, S = torch.empty_like(x["q"]), torch.empty_like(x["S"])
+        binding.darkattn_decay_forward(plan, x["q"], x["k"], x["v"], x["g"], O, plan.alloc_workspace(), S_in=x["S"], S_out=S)
+        torch.cuda.synchronize()
+        alone.append((O, S))
+    streams = [torch.cuda.Stream() for _ in sets]
+    outs = [(torch.zeros_like(x["q"]), torch.zeros_like(x["S"])) for x in sets]
+    spaces = [plan.alloc_workspace() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for x, st, (O, S), ws in zip(sets, streams, outs, spaces):
+            binding.darkattn_decay_forward(plan, x["q"], x["k"], x["v"], x["g"], O, ws, S_in=x["S"], S_out=S, stream=st)
+    torch.cuda.synchronize()
+    for got, want in zip(outs, alone):
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.gpu
+def test_offsets_past_32_bits(binding):
+    """A pool of states, a cache and a batch of rows with more than 2^31 numbers: what lies at their ends comes out as by itself."""
+    H, d = 4, 128
+    n = (1 << 31) // (H * d * d) + 40
+    t = dev(make(2, H, 1, d, seed=70))
+    plan = binding.darkattn_decay_plan(2, H, 1, d)
+    args = [t[x][:, :, 0].contiguous() for x in ("q", "k", "v")]
+    pool = torch.empty(n, H, d, d, device="cuda")
+    slots = torch.tensor([n - 1, 3], dtype=torch.int32, device="cuda")
+    pool[slots.long()] = t["S"]
+    o, o2 = (torch.empty(2, H, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    small = t["S"].clone()
+    binding.darkattn_decay_step(plan, *args, t["g"], pool, o, slots=slots)
+    binding.darkattn_decay_step(plan, *args, t["g"], small, o2)
+    assert torch.equal(o, o2) and torch.equal(pool[slots.long()], small)
+    del pool
+    codes, scales = torch.zeros(n, H, d, d, dtype=torch.int8, device="cuda"), torch.zeros(n, H, d, device="cuda")
+    back, c2, s2 = torch.empty_like(small), torch.zeros(2, H, d, d, dtype=torch.int8, device="cuda"), torch.zeros(2, H, d, device="cuda")
+    binding.darkattn_state_store(small, codes, scales, slots=slots)
+    binding.darkattn_state_store(small, c2, s2)
+    binding.darkattn_state_load(codes, scales, back, slots=slots)
+    assert torch.equal(codes[slots.long()], c2) and torch.equal(scales[slots.long()], s2) and torch.equal(back, c2.float() * s2[..., None])
+    del codes, scales
+    for dtype in ("bf16", "f32"):
+        dt, N, heads = (torch.bfloat16, 1 << 17, 140) if dtype == "bf16" else (torch.float32, 1 << 15, 1025)
+        w = 128 if dtype == "bf16" else 64
+        gen = torch.Generator(device="cuda").manual_seed(1)
+        x = torch.randn(1, heads, N, w, generator=gen, device="cuda", dtype=dt)
+        assert x.numel() > 1 << 31
+        big = binding.darkattn_decay_plan(1, heads, N, w, dtype=binding.BF16 if dtype == "bf16" else binding.F32)
+        g = torch.full((heads,), -0.1, device="cuda")
+        O = torch.empty_like(x)
+        binding.darkattn_decay_forward(big, x, x, x, g, O, big.alloc_workspace())
+        last = x[:, -1:, -700:].cpu()               # what lies before these is decayed by e^-40 where the last 300 are looked at
+        want, _ = oracle_forward(last, last, last, g[:1].cpu(), 1 / math.sqrt(w))
+        mag, _ = oracle_forward(last.abs(), last.abs(), last.abs(), g[:1].cpu(), 1 / math.sqrt(w))
+        check(O[:, -1:, -300:], want[:, :, 400:], mag[:, :, 400:] * (1 + math.exp(-30)), ops_of(w, w, 700), dt, True, "last rows")
+        del x, O
 
 
 @pytest.mark.gpu
