@@ -33,14 +33,16 @@ constexpr int kDiag = 68;                                // numbers of each copy
 struct TcMaps { CUtensorMap x, y, z, o; };
 struct TcArgs { DecayArgs a; TcMaps m[kDecayPasses]; };
 
-enum { FULL0, FULL1, SCORES, INTER, DS, PZ, TMA_BARS, P_READY = TMA_BARS, T_READY, S_READY, O_READ, STAGED, CLEAN, NBARS };
+constexpr int kMostStages = 4;
+enum { FULL, SCORES = FULL + kMostStages, INTER, DS, PZ, TMA_BARS, P_READY = TMA_BARS, T_READY, S_READY, O_READ, STAGED, CLEAN, NBARS };
 
 template <int DY, int DZ, bool MAIN>
 struct TcSmem {
     static constexpr int kX = MAIN ? DY / 64 * 16384 : 0, kY = DY / 64 * 16384, kZ = DZ / 64 * 16384;
-    static constexpr int kStage = kX + kY + kZ;
-    static constexpr int S = 2 * kStage, tok = S + (MAIN ? kZ : 0), near = tok + 512, diag = near + 128, pw = diag + 4 * kDiag * 4, bars = pw + 528, slot = bars + NBARS * 8, total = slot + 16;
-    static_assert(total <= 232448, "shared memory of a block");
+    static constexpr int kStage = kX + kY + kZ, kSpace = 232448 - 2560 - (MAIN ? kZ : 0), kStages = kSpace / kStage < kMostStages ? kSpace / kStage : kMostStages;
+    static constexpr int S = kStages * kStage, tok = S + (MAIN ? kZ : 0), near = tok + 512, diag = near + 128, pw = diag + 4 * kDiag * 4, bars = pw + 528, slot = bars + NBARS * 8, total = slot + 16;
+    static constexpr bool kEarly = MAIN && kZ <= kX;      // rows out are staged in X's place alone: Y and Z can be loaded before they are stored
+    static_assert(kStages >= 2 && total <= 232448, "shared memory of a block");
 };
 
 // tiles of 64 columns and 128 rows of one head: [heads, N, width]
@@ -245,22 +247,29 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         const int at = sp.k0 + (MAIN ? k : nchunk - 1 - k);
         return (reverse ? sp.T - 1 - at : at) * C;
     };
-    const auto load = [&](int it, int k, int g) {         // item `it`: chunk k, head g of those summed over
+    const auto stage_of = [&](int it) { return smem + it % M::kStages * M::kStage; };
+    const auto load_yz = [&](int it, int k, int g) {      // of item `it`: chunk k, head g of those summed over
         if (elect_one()) {
             const TcMaps &m = P.m[ip];
-            unsigned char *stage = smem + (it & 1) * M::kStage;
+            unsigned char *stage = stage_of(it);
+            uint64_t *full = bars + FULL + it % M::kStages;
             const int t0 = first_row(k), hy = hy0 + g;
-            uint64_t *full = bars + FULL0 + (it & 1);
-            mbar_expect_tx(full, M::kStage);
-            if (MAIN) for (int x = 0; x < DY; x += 64) tma_load_3d(stage + x * 256, &m.x, full, x, t0, head);
+            mbar_expect_tx(full, M::kStage);              // (X's bytes among them)
             for (int x = 0; x < DY; x += 64) tma_load_3d(stage + M::kX + x * 256, &m.y, full, x, t0, hy);
             for (int x = 0; x < DZ; x += 64) tma_load_3d(stage + M::kX + M::kY + x * 256, &m.z, full, x, t0, hy);
         }
     };
+    const auto load_x = [&](int it, int k) {
+        if (MAIN && elect_one())
+            for (int x = 0; x < DY; x += 64) tma_load_3d(stage_of(it) + x * 256, &P.m[ip].x, bars + FULL + it % M::kStages, x, first_row(k), head);
+    };
     const bool fine = *abort_flag == 0;
-    if (warp == kWarps && fine) {                         // the first two items' loads, beside the tables
-        if (items > 0) load(0, 0, 0);
-        if (items > 1) load(1, G == 1, G == 1 ? 0 : 1);
+    if (warp == kWarps && fine) {                         // the first items' loads, beside the tables
+        for (int it = 0, k = 0, g = 0; it < M::kStages && it < items; ++it) {
+            load_yz(it, k, g);
+            load_x(it, k);
+            if (++g == G) { g = 0; ++k; }
+        }
     }
     if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
     __syncthreads();
@@ -279,25 +288,32 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         if (tid == 0) atomicExch(status, (int)DARKATTN_ERR_CUDA);
     } else if (warp == kWarps) {                       // ------------------------------------------------ loads and stores
         const TcMaps &m = P.m[ip];
+        // Item by item: its products done, its stage takes the next item's Y and Z; its rows out staged, they are stored, and X follows. (All three
+        // behind the store, and two stages at width 64: a chunk there waited for its loads, 135 us for what now takes XX.)
         bool ok = true;
-        for (int it = 0, k = 0, g = 0, k2 = 0, g2 = 0; it < items + 2 && ok; ++it) {      // (k, g): chunk and head of item `it`, (k2, g2) of the one two before
-            unsigned char *stage = smem + (it & 1) * M::kStage;
-            if (it >= 2) {                                // the stage's tiles have been used, and stored where rows out were staged in them
-                if (MAIN && g2 == G - 1) {
-                    ok = wait_tries(bar + 8 * STAGED, k2 & 1, status);
-                    if (ok && sp.n - first_row(k2) >= C && elect_one()) {
-                        for (int x = 0; x < DZ && x < c; x += 64) tma_store_3d(&m.o, stage + x * 256, x, first_row(k2), head);
-                        tma_store_commit();
-                        tma_store_wait_read();
-                    }
-                } else ok = wait_tries(bar + 8 * (MAIN ? PZ : DS), it & 1, status);
+        int k1 = 0, g1 = 0;                               // chunk and head of the item that goes into the stage
+        for (int it = 0; it < M::kStages && it < items; ++it)
+            if (++g1 == G) { g1 = 0; ++k1; }
+        for (int it = 0, k = 0, g = 0; it < items && ok; ++it) {
+            const int next = it + M::kStages;
+            ok = wait_tries(bar + 8 * (MAIN ? PZ : DS), it & 1, status);
+            if (!ok) break;
+            if ((M::kEarly || !MAIN) && next < items) load_yz(next, k1, g1);
+            if (MAIN && g == G - 1) {
+                ok = wait_tries(bar + 8 * STAGED, k & 1, status);
                 if (!ok) break;
-                if (++g2 == G) { g2 = 0; ++k2; }
+                if (sp.n - first_row(k) >= C && elect_one()) {
+                    for (int x = 0; x < DZ && x < c; x += 64) tma_store_3d(&m.o, stage_of(it) + x * 256, x, first_row(k), head);
+                    tma_store_commit();
+                    tma_store_wait_read();
+                }
             }
-            if (it < items) {
-                if (it >= 2) load(it, k, g);
-                if (++g == G) { g = 0; ++k; }
+            if (next < items) {
+                if (MAIN && !M::kEarly) load_yz(next, k1, g1);
+                load_x(next, k1);
+                if (++g1 == G) { g1 = 0; ++k1; }
             }
+            if (++g == G) { g = 0; ++k; }
         }
         if (MAIN && elect_one()) tma_store_wait_all();
         if (!ok) *abort_flag = 1;
@@ -309,11 +325,11 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         bool ok = true;
         int clean = 0;
         for (int it = 0, k = 0, g = 0; it < items && ok; ++it, k += g + 1 == G, g = g + 1 == G ? 0 : g + 1) {
-            const unsigned char *stage = smem + (it & 1) * M::kStage;
+            const unsigned char *stage = stage_of(it);
             const TileDesc tX(stage), tY(stage + M::kX), tZ(stage + M::kX + M::kY);
             const bool inter = has0 || k > 0;
             if (MAIN) {
-                ok = wait_tries(bar + 8 * (FULL0 + (it & 1)), (it >> 1) & 1, status);
+                ok = wait_tries(bar + 8 * (FULL + it % M::kStages), it / M::kStages & 1, status);
                 if (ok && sp.n - first_row(k) < C) ok = wait_tries(bar + 8 * CLEAN, clean++ & 1, status);
                 if (!ok) break;
                 tc_fence_after();
@@ -405,8 +421,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         uint32_t inters = 0;
         // Brings item `it`'s weighted Y (of a chunk of L rows) into tensor memory.
         const auto prepare = [&](int it, int k, int L) {
-            const uint32_t stage = sbase + (it & 1) * M::kStage;
-            DWAIT(FULL0 + (it & 1), (it >> 1) & 1);
+            const uint32_t stage = sbase + it % M::kStages * M::kStage;
+            DWAIT(FULL + it % M::kStages, it / M::kStages & 1);
             if (L != Ltok || L < C) {
                 warps_bar<32 * kWarps>();                 // the weights of the chunk before have been used
                 for (int i = tid; i < C; i += 32 * kWarps) {
@@ -498,7 +514,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
 #pragma unroll
                         for (int tb = 0; tb < 4 / kGroups; ++tb) {
                             const int t = cb + kGroups * tb;
-                            weighted_transpose<THIRD, kPart>(sbase + (it & 1) * M::kStage + y_own + t * 4096, tok + t * 32 + 2 * (lane & 3), 0, at + kThird + t * 16);
+                            weighted_transpose<THIRD, kPart>(sbase + it % M::kStages * M::kStage + y_own + t * 4096, tok + t * 32 + 2 * (lane & 3), 0, at + kThird + t * 16);
                         }
                     }
                     tmem_wait_st();
@@ -549,7 +565,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 if (g == G - 1) {
                     tc_fence_after();
                     constexpr int kLd = W < 32 ? W : 32;
-                    const uint32_t stage = sbase + (it & 1) * M::kStage + own;
+                    const uint32_t stage = sbase + it % M::kStages * M::kStage + own;
 #pragma unroll
                     for (int h = 0; h < W; h += kLd) {
                         uint32_t o[kLd];
