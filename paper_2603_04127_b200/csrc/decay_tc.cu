@@ -34,7 +34,9 @@ struct TcMaps { CUtensorMap x, y, z, o; };
 struct TcArgs { DecayArgs a; TcMaps m[kDecayPasses]; };
 
 constexpr int kMostStages = 4;
-enum { FULL, SCORES = FULL + kMostStages, INTER, DS, PZ, TMA_BARS, P_READY = TMA_BARS, T_READY, S_READY, O_READ, STAGED, CLEAN, NBARS };
+// A wait sees one bit of a barrier's count, so nobody may be two phases behind. The products and the warps between them wait for one another item by
+// item; the warp that loads and stores does not hold them up until they need a stage from it, so what it waits for has a barrier for each stage.
+enum { FULL, DS = FULL + kMostStages, PZ = DS + kMostStages, SCORES = PZ + kMostStages, INTER, TMA_BARS, P_READY = TMA_BARS, T_READY, S_READY, O_READ, CLEAN, STAGED, NBARS = STAGED + kMostStages };
 
 template <int DY, int DZ, bool MAIN>
 struct TcSmem {
@@ -289,18 +291,18 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     } else if (warp == kWarps) {                       // ------------------------------------------------ loads and stores
         const TcMaps &m = P.m[ip];
         // Item by item: its products done, its stage takes the next item's Y and Z; its rows out staged, they are stored, and X follows. (All three
-        // behind the store, and two stages at width 64: a chunk there waited for its loads, 135 us for what now takes XX.)
+        // behind the store, and two stages at width 64: a chunk there waited for its loads, 135 us for what now takes 125.)
         bool ok = true;
         int k1 = 0, g1 = 0;                               // chunk and head of the item that goes into the stage
         for (int it = 0; it < M::kStages && it < items; ++it)
             if (++g1 == G) { g1 = 0; ++k1; }
         for (int it = 0, k = 0, g = 0; it < items && ok; ++it) {
             const int next = it + M::kStages;
-            ok = wait_tries(bar + 8 * (MAIN ? PZ : DS), it & 1, status);
+            ok = wait_tries(bar + 8 * ((MAIN ? PZ : DS) + it % M::kStages), it / M::kStages & 1, status);
             if (!ok) break;
             if ((M::kEarly || !MAIN) && next < items) load_yz(next, k1, g1);
             if (MAIN && g == G - 1) {
-                ok = wait_tries(bar + 8 * STAGED, k & 1, status);
+                ok = wait_tries(bar + 8 * (STAGED + k % M::kStages), k / M::kStages & 1, status);
                 if (!ok) break;
                 if (sp.n - first_row(k) >= C && elect_one()) {
                     for (int x = 0; x < DZ && x < c; x += 64) tma_store_3d(&m.o, stage_of(it) + x * 256, x, first_row(k), head);
@@ -366,7 +368,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     for (int q = 0; q < (kHalves ? 4 : 8); ++q)
                         mma_ts(tmem + kD, left + 8 * q, kHalves ? halves + (uint64_t)(q * 2048 >> 4) : mndesc(tZ, q), id_d, g > 0 || part > 0 || q > 0);
                 }
-                mma_commit(bars + DS);
+                mma_commit(bars + DS + it % M::kStages);
             }
             if (MAIN) {
                 ok = wait_tries(bar + 8 * P_READY, it & 1, status);
@@ -375,7 +377,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 if (elect_one()) {
 #pragma unroll
                     for (int q = 0; q < 8; ++q) mma_ts(tmem + kO, tmem + kA + 8 * q, mndesc(tZ, q), id_z, (DZ == 128 && inter) || g > 0 || q > 0);
-                    mma_commit(bars + PZ);
+                    mma_commit(bars + PZ + it % M::kStages);
                 }
             }
         }
@@ -542,7 +544,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 tc_fence_before();
                 arrive_warp(bar + 8 * P_READY, lane);
             }
-            if (k < kept) DWAIT(DS, it & 1);
+            if (k < kept) DWAIT(DS + it % M::kStages, it / M::kStages & 1);
             if (k < kept && g == G - 1) {
                 tc_fence_after();
                 const float keep = MAIN ? pw[L] : 1.f, share = behind;
@@ -561,7 +563,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 arrive_warp(bar + 8 * S_READY, lane);
             }
             if (MAIN) {
-                DWAIT(PZ, it & 1);
+                DWAIT(PZ + it % M::kStages, it / M::kStages & 1);
                 if (g == G - 1) {
                     tc_fence_after();
                     constexpr int kLd = W < 32 ? W : 32;
@@ -590,7 +592,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                         }
                     }
                     fence_async_smem();
-                    arrive_warp(bar + 8 * STAGED, lane);
+                    arrive_warp(bar + 8 * (STAGED + k % M::kStages), lane);
                 }
             }
             if (++g == G) { g = 0; ++k; }
