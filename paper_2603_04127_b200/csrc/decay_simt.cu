@@ -1,7 +1,7 @@
 // Attention with a decay per head in FP32 arithmetic: any width up to 512, any length, fp32 or bf16 in memory.
 //
 // A block takes a segment of one head's chunks in the pass's order (64 rows a chunk), per chunk four products: scores X Y^T, X S, the
-// state's update Y^T Z, and P Z. Widths up to 128 have kernels of their own below; wider ones go by slices of 64 and tiles of TZ columns
+// state's update Y^T Z, and P Z. Widths up to 128 have kernels of their own below; wider ones go by slices of 64 and tiles of 64 columns
 // of the output, whose share of the state stays in shared memory for the whole segment.
 #include "decay.cuh"
 
@@ -19,40 +19,30 @@ template <typename T> __device__ __forceinline__ T from_f(float x);
 template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-template <int TZ>
 struct SimtSmem {
-    static constexpr int XT = 0, YT = XT + F * kPad, Yr = YT + F * kPad, Z = Yr + C * F, PT = Z + C * TZ, pw = PT + C * kPad, S = pw + 72;
-    static int bytes(int a) { return (S + (a + F - 1) / F * F * TZ) * 4; }
+    static constexpr int XT = 0, YT = XT + F * kPad, Yr = YT + F * kPad, Z = Yr + C * F, PT = Z + C * F, pw = PT + C * kPad, S = pw + 72;
+    static int bytes(int a) { return (S + (a + F - 1) / F * F * F) * 4; }
 };
 
-__device__ __forceinline__ int zcol(int tx, int v) { return v < 4 ? tx * 4 + v : 64 + tx * 4 + v - 4; }
-
-// acc[4][RZ] += sum_k A[k][ty*4 ..] B[k][columns of tx]
-template <int RZ, int K>
-__device__ __forceinline__ void outer(float (&acc)[4][RZ], const float *A, int lda, const float *B, int ldb, int ty, int tx)
+// acc += sum over k < 64 of A[k][ty * 4 ..] B[k][tx * 4 ..]
+__device__ __forceinline__ void outer(float (&acc)[4][4], const float *A, int lda, const float *B, int ldb, int ty, int tx)
 {
 #pragma unroll 8
-    for (int k = 0; k < K; ++k) {
-        const float4 x = *reinterpret_cast<const float4 *>(A + k * lda + ty * 4);
-        float y[RZ];
+    for (int k = 0; k < 64; ++k) {
+        const float4 x = *reinterpret_cast<const float4 *>(A + k * lda + ty * 4), y = *reinterpret_cast<const float4 *>(B + k * ldb + tx * 4);
+        const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-        for (int q = 0; q < RZ / 4; ++q) *reinterpret_cast<float4 *>(y + 4 * q) = *reinterpret_cast<const float4 *>(B + k * ldb + q * 64 + tx * 4);
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int v = 0; v < RZ; ++v) {
-            acc[0][v] = fmaf(x.x, y[v], acc[0][v]);
-            acc[1][v] = fmaf(x.y, y[v], acc[1][v]);
-            acc[2][v] = fmaf(x.z, y[v], acc[2][v]);
-            acc[3][v] = fmaf(x.w, y[v], acc[3][v]);
-        }
+            for (int v = 0; v < 4; ++v) acc[u][v] = fmaf(xs[u], ys[v], acc[u][v]);
     }
 }
 
 // MAIN: rows out; otherwise only the state of each of the first nseg - 1 segments, from zero, into pass.seg
-template <typename T, int TZ, bool MAIN>
+template <typename T, bool MAIN>
 __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_constant__ DecayArgs A, int ntz)
 {
-    constexpr int RZ = TZ / 16;
-    using M = SimtSmem<TZ>;
+    using M = SimtSmem;
     extern __shared__ __align__(16) float sm[];
     float *XT = sm + M::XT, *YT = sm + M::YT, *Yr = sm + M::Yr, *Zs = sm + M::Z, *PT = sm + M::PT, *pw = sm + M::pw, *S = sm + M::S;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
@@ -64,7 +54,7 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
     const DecayPass &p = A.pass[id % A.npass]; id /= A.npass;
     const int zt = id % ntz; id /= ntz;
     const int seg = id % nseg, head = id / nseg;            // head: of X, or of the state
-    const int z0 = zt * TZ;
+    const int z0 = zt * F;
     if (z0 >= p.c) return;
     const int HX = MAIN ? p.HX : A.Hkv;
     const int b = head / HX, hx = head % HX;
@@ -81,8 +71,8 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
     if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
     const float *S_in = nullptr;
     if (MAIN) S_in = seg == 0 ? (p.S_in ? p.S_in + (size_t)(b * A.Hkv + hs) * a * c : nullptr) : p.seg + ((size_t)(b * A.Hkv + hs) * (nseg - 1) * A.sub + seg * A.sub - 1) * a * c;
-    for (int i = tid; i < nf * F * TZ; i += kThreadsS) {
-        const int f = i / TZ, z = z0 + i % TZ;
+    for (int i = tid; i < nf * F * F; i += kThreadsS) {
+        const int f = i / F, z = z0 + i % F;
         S[i] = S_in && f < a && z < c ? (p.trans ? S_in[(size_t)z * a + f] : S_in[(size_t)f * c + z]) : 0.f;
     }
     const T *X = static_cast<const T *>(p.X) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * a;
@@ -90,18 +80,14 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
 
     for (int k = sp.k0; k < sp.k1; ++k) {
         const int t0 = (p.reverse ? sp.T - 1 - k : k) * C, L = min(C, sp.n - t0);
-        float o[4][RZ];
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int v = 0; v < RZ; ++v) o[u][v] = 0.f;
+        float o[4][4] = {};
         for (int g = 0; g < G; ++g) {
             const T *Y = static_cast<const T *>(p.Y) + ((size_t)(b * p.HY + hy0 + g) * A.N + t0) * a;
             const T *Z = static_cast<const T *>(p.Z) + ((size_t)(b * p.HY + hy0 + g) * A.N + t0) * c;
             float sc[4][4] = {};
             __syncthreads();                                 // the tiles of the step before have been read, pw and S are there
-            for (int i = tid; i < C * TZ; i += kThreadsS) {
-                const int r = i / TZ, z = z0 + i % TZ;
+            for (int i = tid; i < C * F; i += kThreadsS) {
+                const int r = i / F, z = z0 + i % F;
                 Zs[i] = r < L && z < c ? to_f(Z[(size_t)r * c + z]) : 0.f;
             }
             for (int fs = 0; fs < nf; ++fs) {
@@ -117,23 +103,19 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
                     Yr[r * F + fl] = in ? y * (pw[p.reverse ? r + 1 : L - 1 - r] * p.tok_mul) : 0.f;
                 }
                 __syncthreads();
-                float d[4][RZ];
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-#pragma unroll
-                    for (int v = 0; v < RZ; ++v) d[u][v] = 0.f;
+                float d[4][4] = {};
                 if (MAIN) {
-                    outer<4, F>(sc, XT, kPad, YT, kPad, ty, tx);
-                    if (g == 0) outer<RZ, F>(o, XT, kPad, S + fs * F * TZ, TZ, ty, tx);
+                    outer(sc, XT, kPad, YT, kPad, ty, tx);
+                    if (g == 0) outer(o, XT, kPad, S + fs * F * F, F, ty, tx);
                 }
-                outer<RZ, C>(d, Yr, F, Zs, TZ, ty, tx);
+                outer(d, Yr, F, Zs, F, ty, tx);
                 if (MAIN && g == 0) __syncthreads();         // the state before this chunk has been read
                 const float keep = g == 0 ? pw[L] : 1.f;
 #pragma unroll
                 for (int u = 0; u < 4; ++u)
 #pragma unroll
-                    for (int v = 0; v < RZ; ++v) {
-                        float &s = S[(fs * F + ty * 4 + u) * TZ + zcol(tx, v)];
+                    for (int v = 0; v < 4; ++v) {
+                        float &s = S[(fs * F + ty * 4 + u) * F + tx * 4 + v];
                         s = keep * s + d[u][v];
                     }
             }
@@ -144,7 +126,7 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
                     const int r = ty * 4 + u;
                     const float m = r < L ? pw[p.reverse ? L - 1 - r : r + 1] * p.row_mul : 0.f;
 #pragma unroll
-                    for (int v = 0; v < RZ; ++v) o[u][v] *= m;
+                    for (int v = 0; v < 4; ++v) o[u][v] *= m;
                 }
             }
 #pragma unroll
@@ -155,7 +137,7 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
                     PT[(tx * 4 + v) * kPad + ty * 4 + u] = n >= 0 ? sc[u][v] * (pw[n] * p.p_mul) : 0.f;
                 }
             __syncthreads();
-            outer<RZ, C>(o, PT, kPad, Zs, TZ, ty, tx);
+            outer(o, PT, kPad, Zs, F, ty, tx);
         }
         if (MAIN) {
 #pragma unroll
@@ -163,8 +145,8 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
                 const int r = ty * 4 + u;
                 if (r >= L) continue;
 #pragma unroll
-                for (int v = 0; v < RZ; ++v) {
-                    const int z = z0 + zcol(tx, v);
+                for (int v = 0; v < 4; ++v) {
+                    const int z = z0 + tx * 4 + v;
                     if (z < c) O[(size_t)(t0 + r) * c + z] = from_f<T>(o[u][v]);
                 }
             }
@@ -172,8 +154,8 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
     }
     if (S_out) {
         __syncthreads();
-        for (int i = tid; i < a * TZ; i += kThreadsS) {
-            const int f = i / TZ, z = z0 + i % TZ;
+        for (int i = tid; i < a * F; i += kThreadsS) {
+            const int f = i / F, z = z0 + i % F;
             if (z < c) S_out[(size_t)f * c + z] = S[i];
         }
     }
@@ -501,8 +483,8 @@ cudaError_t launch_tile(const DecayArgs &A, cudaStream_t st)
     return cudaGetLastError();
 }
 
-template <typename T, int TZ, bool MAIN>
-cudaError_t launch(const DecayArgs &A, cudaStream_t st)
+template <typename T, bool MAIN>
+cudaError_t launch_wide(const DecayArgs &A, cudaStream_t st)
 {
     int a = 0, c = 0, heads = 0;
     for (int i = 0; i < A.npass; ++i) {
@@ -510,8 +492,8 @@ cudaError_t launch(const DecayArgs &A, cudaStream_t st)
         c = max(c, A.pass[i].c);
         heads = max(heads, MAIN ? A.B * A.pass[i].HX : A.B * A.Hkv);
     }
-    const int ntz = (c + TZ - 1) / TZ, nseg = MAIN ? A.nseg : A.nseg - 1;
-    return launch_pdl(decay_simt_kernel<T, TZ, MAIN>, dim3((unsigned)((long long)A.npass * ntz * nseg * heads)), dim3(kThreadsS), SimtSmem<TZ>::bytes(a), st, A, ntz);
+    const int ntz = (c + F - 1) / F, nseg = MAIN ? A.nseg : A.nseg - 1;
+    return launch_pdl(decay_simt_kernel<T, MAIN>, dim3((unsigned)((long long)A.npass * ntz * nseg * heads)), dim3(kThreadsS), SimtSmem::bytes(a), st, A, ntz);
 }
 
 template <typename T, bool MAIN>
@@ -521,7 +503,7 @@ cudaError_t launch_t(const DecayArgs &A, cudaStream_t st)
     for (int i = 0; i < A.npass; ++i) { a = max(a, A.pass[i].a); c = max(c, A.pass[i].c); }
     const int w = max(a, c);
     return w <= 64 ? launch_tile<T, 4, MAIN>(A, st) : w <= 80 ? launch_tile<T, 5, MAIN>(A, st) : w <= 96 ? launch_tile<T, 6, MAIN>(A, st)
-           : w <= 128 ? launch_tile<T, 8, MAIN>(A, st) : launch<T, 64, MAIN>(A, st);
+           : w <= 128 ? launch_tile<T, 8, MAIN>(A, st) : launch_wide<T, MAIN>(A, st);
 }
 
 }  // namespace
