@@ -240,7 +240,9 @@ darkattn_status_t darkattn_forward_static(darkattn_plan_t plan, const void *Q, c
  *                                  they were, those of dQ, dK and dV are set to zero.
  *
  * Conventions as at the top of this file (contiguous, 16-byte aligned - log_decay, lengths and slots 4 -, caller-owned,
- * asynchronous on the stream, nothing allocated). Inputs have to be finite: what is not spreads to its whole chunk. */
+ * asynchronous on the stream, nothing allocated). Inputs have to be finite: what is not spreads to its whole chunk. What a call writes
+ * must overlap nothing else that it reads or writes (DARKATTN_ERR_INVALID_ARG). Calls whose GPU work may run at the same time
+ * (on two streams, or as two captured graphs) need a workspace each; a plan may serve any number of them. */
 typedef struct {
     int32_t B, H, N;      /* batch, query heads, (padded) sequence length; all >= 1, B H <= 65535             */
     int32_t d;            /* query/key width, 1 .. 512                                                          */
@@ -260,15 +262,15 @@ int32_t darkattn_decay_plan_path(darkattn_decay_plan_t plan);
 void darkattn_decay_destroy(darkattn_decay_plan_t plan);
 
 /* The chunked form: a whole (batch of) prompt(s). S_in: the state before the first token, or NULL. S_out: receives the state
- * behind the last token of each sequence, or NULL; must not overlap S_in. Sequences are cut into segments where there are too
+ * behind the last token of each sequence, or NULL. Sequences are cut into segments where there are too
  * few heads for the GPU; the states between them live in the workspace.                                      */
 darkattn_status_t darkattn_decay_forward(darkattn_decay_plan_t plan, const void *Q, const void *K, const void *V, const float *log_decay,
                                          const int32_t *lengths /* nullable */, const float *S_in /* nullable */, void *O,
                                          float *S_out /* nullable */, void *workspace, void *cuda_stream);
 
 /* Gradients of L = sum(dO .* O) + sum(dS_out .* S_out): dS_out is the gradient with respect to the state behind the last
- * token (NULL: zero), dS_in receives the one with respect to the state before the first (NULL: not wanted; must overlap
- * neither dS_out nor S_in). dK, dV and dS_in sum over the query heads of a group. Needs nothing from the forward pass.   */
+ * token (NULL: zero), dS_in receives the one with respect to the state before the first (NULL: not wanted).
+ * dK, dV and dS_in sum over the query heads of a group. Needs nothing from the forward pass.   */
 darkattn_status_t darkattn_decay_backward(darkattn_decay_plan_t plan, const void *Q, const void *K, const void *V, const float *log_decay,
                                           const int32_t *lengths /* nullable */, const float *S_in /* nullable */, const void *dO,
                                           const float *dS_out /* nullable */, void *dQ, void *dK, void *dV, float *dS_in /* nullable */,
@@ -291,10 +293,10 @@ darkattn_status_t darkattn_decay_last_device_status(darkattn_decay_plan_t plan, 
  * scale = max |x| / top in float32, code = x / scale rounded to nearest (ties to even) from the exact quotient.
  *   I8   : signed integers, top = 127; off by at most max |x| / 254
  *   E4M3 : 8-bit floating point, top = 448; off by at most 2^-4 of the value, or max |x| / 458752 where that is more
- * A row that holds an infinity or NaN is read back as NaN throughout.
+ * (with max |x| above 1e-35: below, the scale has fewer bits). A row that holds an infinity or NaN is read back as NaN throughout.
  *   S [B, rows, cols] float32;  codes [n_slots, rows, cols] one byte each;  scales [n_slots, rows] float32
- * (rows: heads times the state's rows). Sequence b is kept in slot slots[b] (b where slots is NULL). Padding as in
- * darkattn_decay_step: rows whose slot is out of range, and for the store those whose slot an earlier row has named.    */
+ * (rows: heads times the state's rows; B <= 65535, rows and cols <= 2^30). Sequence b is kept in slot slots[b] (b where
+ * slots is NULL); no array overlaps another. Padding as in darkattn_decay_step: rows whose slot is out of range, and for the store those whose slot an earlier row has named.    */
 typedef enum { DARKATTN_STATE_I8 = 0, DARKATTN_STATE_E4M3 = 1 } darkattn_state_format_t;
 darkattn_status_t darkattn_state_store(int32_t B, int32_t rows, int32_t cols, const float *S, const int32_t *slots /* nullable */,
                                        int32_t n_slots, int32_t format, void *codes, float *scales, void *cuda_stream);

@@ -15,6 +15,8 @@
 
 #include "common.cuh"
 
+#include <initializer_list>
+
 namespace darkattn {
 
 struct DecayPass {
@@ -80,6 +82,26 @@ struct darkattn_decay_plan_s {
 };
 
 namespace darkattn {
+
+// Arrays of a call, on the host. What a call writes must not lie over anything else that it reads or writes: blocks take rows in any order.
+struct Span {
+    const void *p;
+    size_t bytes;
+};
+inline bool clash(std::initializer_list<Span> out, std::initializer_list<Span> in)
+{
+    const auto meet = [](const Span &a, const Span &b) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+        return a.p && b.p && x < y + b.bytes && y < x + a.bytes;
+    };
+    for (const Span *o = out.begin(); o != out.end(); ++o) {
+        for (const Span *p = out.begin(); p != o; ++p)
+            if (meet(*o, *p)) return true;
+        for (const Span &i : in)
+            if (meet(*o, i)) return true;
+    }
+    return false;
+}
 
 // FP32 kernels, any shape
 void decay_simt_split(darkattn_decay_plan_s *plan);

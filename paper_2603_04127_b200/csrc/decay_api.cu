@@ -11,25 +11,32 @@ template <typename... P> static bool all_set(const P *...p) { return ((p != null
 template <typename... P> static bool all_aligned(const P *...p) { return (aligned16(p) && ...); }
 static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-static bool overlap(const void *p, const void *q, size_t bytes)
-{
-    if (!p || !q) return false;
-    const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
-    return x < y + bytes && y < x + bytes;
-}
+// bytes of the arrays of a call
+struct Sizes {
+    size_t q, k, v, o, s, g, n;
+    explicit Sizes(const darkattn_decay_desc_t &ds)
+    {
+        const size_t e = ds.dtype == DARKATTN_BF16 ? 2 : 4, rows = (size_t)ds.B * ds.N * e;
+        q = rows * ds.H * ds.d; k = rows * ds.H_kv * ds.d; v = rows * ds.H_kv * ds.dv; o = rows * ds.H * ds.dv;
+        s = (size_t)ds.B * ds.H_kv * ds.d * ds.dv * 4; g = (size_t)ds.H_kv * 4; n = (size_t)ds.B * 4;
+    }
+};
 
 // Rows of the gradients behind a sequence's end: zero.
 __global__ void __launch_bounds__(256) decay_zero_tail_kernel(unsigned char *dQ, unsigned char *dK, unsigned char *dV, const int *lengths, int H, int Hkv,
                                                              int N, int row_d, int row_dv)
 {
+    // (16 bytes at a time where rows are multiples of that)
     pdl_wait();
     const int b = blockIdx.y, n = min(max(lengths[b], 0), N), which = blockIdx.z;
     unsigned char *p = which == 0 ? dQ : which == 1 ? dK : dV;
     const int heads = which == 0 ? H : Hkv, row = which == 2 ? row_dv : row_d;
-    const long long per = (long long)(N - n) * row / 2;      // 16-bit words of a head
+    const bool wide = row % 16 == 0;
+    const long long bytes = (long long)(N - n) * row;        // of a head
     for (int h = blockIdx.x; h < heads; h += gridDim.x) {
-        unsigned short *at = reinterpret_cast<unsigned short *>(p + ((long long)(b * heads + h) * N + n) * row);
-        for (long long i = threadIdx.x; i < per; i += 256) at[i] = 0;
+        unsigned char *at = p + ((long long)(b * heads + h) * N + n) * row;
+        if (wide) for (long long i = threadIdx.x; i < bytes / 16; i += 256) reinterpret_cast<uint4 *>(at)[i] = make_uint4(0, 0, 0, 0);
+        else for (long long i = threadIdx.x; i < bytes / 2; i += 256) reinterpret_cast<unsigned short *>(at)[i] = 0;
     }
 }
 
@@ -102,7 +109,8 @@ darkattn_status_t darkattn_decay_forward(darkattn_decay_plan_t plan, const void 
     if (!workspace) return DARKATTN_ERR_WORKSPACE;
     if (!all_aligned(Q, K, V, O, workspace) || !all_aligned(S_in, S_out) || !aligned4(log_decay) || !aligned4(lengths)) return DARKATTN_ERR_INVALID_ARG;
     const darkattn_decay_desc_t &ds = plan->desc;
-    if (overlap(S_in, S_out, (size_t)ds.B * ds.H_kv * ds.d * ds.dv * sizeof(float))) return DARKATTN_ERR_INVALID_ARG;
+    const Sizes z(ds);
+    if (clash({{O, z.o}, {S_out, z.s}, {workspace, plan->workspace_bytes}}, {{Q, z.q}, {K, z.k}, {V, z.v}, {log_decay, z.g}, {lengths, z.n}, {S_in, z.s}})) return DARKATTN_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     DecayArgs A = common_args(plan, log_decay, lengths, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub, workspace);
     float *seg = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->ws.seg[0]);
@@ -120,8 +128,9 @@ darkattn_status_t darkattn_decay_backward(darkattn_decay_plan_t plan, const void
     if (!workspace) return DARKATTN_ERR_WORKSPACE;
     if (!all_aligned(Q, K, V, dO, dQ, dK, dV, workspace) || !all_aligned(S_in, dS_out, dS_in) || !aligned4(log_decay) || !aligned4(lengths)) return DARKATTN_ERR_INVALID_ARG;
     const darkattn_decay_desc_t &ds = plan->desc;
-    const size_t states = (size_t)ds.B * ds.H_kv * ds.d * ds.dv * sizeof(float);
-    if (overlap(dS_out, dS_in, states) || overlap(S_in, dS_in, states)) return DARKATTN_ERR_INVALID_ARG;
+    const Sizes z(ds);
+    if (clash({{dQ, z.q}, {dK, z.k}, {dV, z.v}, {dS_in, z.s}, {workspace, plan->workspace_bytes}},
+              {{Q, z.q}, {K, z.k}, {V, z.v}, {log_decay, z.g}, {lengths, z.n}, {S_in, z.s}, {dO, z.o}, {dS_out, z.s}})) return DARKATTN_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     DecayArgs A = common_args(plan, log_decay, lengths, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub, workspace);
     float *S = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->ws.seg[0]), *R = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan->ws.seg[1]);

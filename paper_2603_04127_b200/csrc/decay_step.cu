@@ -252,9 +252,12 @@ darkattn_status_t decay_step(const darkattn_decay_plan_s *plan, const void *q, c
     const darkattn_decay_desc_t &ds = plan->desc;
     // shared memory of the narrowest block: the queries of a group and their sums
     if (4ll * ((ds.H / ds.H_kv) * (ds.d + kWarps * 32) + ds.d) > 200 * 1024) return DARKATTN_ERR_UNSUPPORTED;
-    const cudaError_t e = ds.dtype == DARKATTN_BF16 ? launch_t<__nv_bfloat16>(ds, q, k, v, log_decay, S, slots, n_slots, o, st)
+    const size_t e = ds.dtype == DARKATTN_BF16 ? 2 : 4, B = (size_t)ds.B;
+    if (clash({{o, B * ds.H * ds.dv * e}, {S, (size_t)n_slots * ds.H_kv * ds.d * ds.dv * 4}},
+              {{q, B * ds.H * ds.d * e}, {k, B * ds.H_kv * ds.d * e}, {v, B * ds.H_kv * ds.dv * e}, {log_decay, (size_t)ds.H_kv * 4}, {slots, B * 4}})) return DARKATTN_ERR_INVALID_ARG;
+    const cudaError_t rc = ds.dtype == DARKATTN_BF16 ? launch_t<__nv_bfloat16>(ds, q, k, v, log_decay, S, slots, n_slots, o, st)
                                                     : launch_t<float>(ds, q, k, v, log_decay, S, slots, n_slots, o, st);
-    DARKATTN_CUDA_TRY(e, "decay_step_kernel");
+    DARKATTN_CUDA_TRY(rc, "decay_step_kernel");
     return DARKATTN_OK;
 }
 

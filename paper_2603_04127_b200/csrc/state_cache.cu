@@ -4,7 +4,7 @@
 // the rounding to the code's few bits sees on which side of a border the exact quotient lies.
 //
 // Bound by the traffic, 5 bytes an element; a warp takes four rows at a time, so that enough loads are on their way.
-#include "common.cuh"
+#include "decay.cuh"
 
 #include <cuda_fp8.h>
 #include <float.h>
@@ -199,13 +199,16 @@ cudaError_t load(const unsigned char *codes, const float *scales, const int *slo
                 : launch_pdl(state_load_kernel<false, V, L>, grid, dim3(kWarps * 32), 0, st, codes, scales, slots, n_slots, rows, cols, S);
 }
 
-darkattn_status_t check(int B, int rows, int cols, int n_slots, int format, const void *S, const void *codes, const void *scales, const void *slots)
+darkattn_status_t check(int B, int rows, int cols, int n_slots, int format, const void *S, const void *codes, const void *scales, const void *slots, bool store)
 {
     const auto low = [](const void *p) { return reinterpret_cast<uintptr_t>(p) & 15u; };
     if (B < 1 || rows < 1 || cols < 1 || n_slots < 1 || (!slots && n_slots < B) || !S || !codes || !scales) return DARKATTN_ERR_INVALID_ARG;
     if (format != DARKATTN_STATE_I8 && format != DARKATTN_STATE_E4M3) return DARKATTN_ERR_INVALID_ARG;
     if (low(S) || low(codes) || low(scales) || (low(slots) & 3u)) return DARKATTN_ERR_INVALID_ARG;
-    return B > 65535 ? DARKATTN_ERR_UNSUPPORTED : DARKATTN_OK;
+    if (B > 65535 || rows > 1 << 30 || cols > 1 << 30) return DARKATTN_ERR_UNSUPPORTED;       // (a row's and a column's index in 32 bits, a block's step behind the end too)
+    const size_t r = (size_t)rows, c = (size_t)cols;
+    const Span state = {S, B * r * c * 4}, kept = {codes, n_slots * r * c}, scale = {scales, n_slots * r * 4}, at = {slots, (size_t)B * 4};
+    return (store ? clash({kept, scale}, {state, at}) : clash({state}, {kept, scale, at})) ? DARKATTN_ERR_INVALID_ARG : DARKATTN_OK;
 }
 
 }  // namespace
@@ -218,7 +221,7 @@ extern "C" {
 darkattn_status_t darkattn_state_store(int32_t B, int32_t rows, int32_t cols, const float *S, const int32_t *slots, int32_t n_slots, int32_t format, void *codes,
                                        float *scales, void *cuda_stream)
 {
-    if (darkattn_status_t rc = check(B, rows, cols, n_slots, format, S, codes, scales, slots)) return rc;
+    if (darkattn_status_t rc = check(B, rows, cols, n_slots, format, S, codes, scales, slots, true)) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     unsigned char *c = static_cast<unsigned char *>(codes);
     const cudaError_t e = cols % 4 || cols > 256 ? store<0, 32>(S, slots, n_slots, B, rows, cols, format, c, scales, st)
@@ -233,7 +236,7 @@ darkattn_status_t darkattn_state_store(int32_t B, int32_t rows, int32_t cols, co
 darkattn_status_t darkattn_state_load(int32_t B, int32_t rows, int32_t cols, const void *codes, const float *scales, const int32_t *slots, int32_t n_slots, int32_t format,
                                       float *S, void *cuda_stream)
 {
-    if (darkattn_status_t rc = check(B, rows, cols, n_slots, format, S, codes, scales, slots)) return rc;
+    if (darkattn_status_t rc = check(B, rows, cols, n_slots, format, S, codes, scales, slots, false)) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const unsigned char *c = static_cast<const unsigned char *>(codes);
     const cudaError_t e = cols % 4 || cols > 256 ? load<0, 32>(c, scales, slots, n_slots, B, rows, cols, format, S, st)

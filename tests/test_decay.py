@@ -241,6 +241,50 @@ def test_calls_refuse_before_launch(binding):
         x.destroy()
 
 
+def test_arrays_that_overlap_are_refused(binding):
+    p = binding.darkattn_decay_plan(2, 4, 100, 64, H_kv=2)
+    lib = binding.lib
+    at = [(i + 1) << 24 for i in range(14)]                     # no two of them overlap; each is refused before anything is launched
+    rows = 2 * 4 * 100 * 64 * 2
+    fwd = [*at[:4], None, at[4], at[5], at[6], at[7], None]     # Q K V log_decay lengths S_in O S_out workspace
+    for out in (6, 7, 8):
+        for other in (0, 1, 2, 3, 5, 6, 7, 8):
+            if out != other:
+                x = list(fwd)
+                x[out] = x[other] + 16 if other != 3 else x[other]
+                assert lib.darkattn_decay_forward(p.handle, *x) == binding.ERR_INVALID_ARG, (out, other)
+    x = list(fwd)
+    x[6] = x[0] - rows + 16                                     # from below
+    assert lib.darkattn_decay_forward(p.handle, *x) == binding.ERR_INVALID_ARG
+    bwd = [*at[:4], None, *at[4:12], None]                      # Q K V log_decay lengths S_in dO dS_out dQ dK dV dS_in workspace
+    for out in range(8, 13):
+        for other in (0, 1, 2, 3, 5, 6, 7, 8, 9, 10, 11, 12):
+            if out != other:
+                x = list(bwd)
+                x[out] = x[other]
+                assert lib.darkattn_decay_backward(p.handle, *x) == binding.ERR_INVALID_ARG, (out, other)
+    step = [*at[:5], at[5], 2, at[6], None]                     # q k v log_decay S slots n_slots o
+    for out in (4, 7):
+        for other in (0, 1, 2, 3, 4, 5, 7):
+            if out != other:
+                x = list(step)
+                x[out] = x[other]
+                assert lib.darkattn_decay_step(p.handle, *x) == binding.ERR_INVALID_ARG, (out, other)
+    a, b, c, s = at[:4]
+    for x in ((a, s, a, c), (a, s, b, a), (a, s, s, c), (a, s, b, s), (a, s, b, b)):
+        assert lib.darkattn_state_store(2, 8, 8, x[0], x[1], 4, 0, x[2], x[3], None) == binding.ERR_INVALID_ARG
+    for x in ((b, c, s, b), (b, c, s, c), (b, c, s, s)):
+        assert lib.darkattn_state_load(2, 8, 8, x[0], x[1], x[2], 4, 0, x[3], None) == binding.ERR_INVALID_ARG
+    p.destroy()
+
+
+@pytest.mark.parametrize("rows,cols", [((1 << 30) + 1, 1), (2 ** 31 - 1, 8), (1, (1 << 30) + 1), (1, 2 ** 31 - 1)])
+def test_cache_sizes_whose_indices_would_wrap_are_refused(binding, rows, cols):
+    a, b, c = 1 << 45, 1 << 46, 1 << 47
+    assert binding.lib.darkattn_state_store(1, rows, cols, a, None, 1, 0, b, c, None) == binding.ERR_UNSUPPORTED
+    assert binding.lib.darkattn_state_load(1, rows, cols, b, c, None, 1, 0, a, None) == binding.ERR_UNSUPPORTED
+
+
 def test_the_oracle_is_the_quadratic_form():
     t = make(2, 4, 37, 6, dv=5, Hk=2, dtype="f32")
     q, k, v = (t[x].double() for x in ("q", "k", "v"))
