@@ -22,24 +22,6 @@ struct Sizes {
     }
 };
 
-// Rows of the gradients behind a sequence's end: zero.
-__global__ void __launch_bounds__(256) decay_zero_tail_kernel(unsigned char *dQ, unsigned char *dK, unsigned char *dV, const int *lengths, int H, int Hkv,
-                                                             int N, int row_d, int row_dv)
-{
-    // (16 bytes at a time where rows are multiples of that)
-    pdl_wait();
-    const int b = blockIdx.y, n = min(max(lengths[b], 0), N), which = blockIdx.z;
-    unsigned char *p = which == 0 ? dQ : which == 1 ? dK : dV;
-    const int heads = which == 0 ? H : Hkv, row = which == 2 ? row_dv : row_d;
-    const bool wide = row % 16 == 0;
-    const long long bytes = (long long)(N - n) * row;        // of a head
-    for (int h = blockIdx.x; h < heads; h += gridDim.x) {
-        unsigned char *at = p + ((long long)(b * heads + h) * N + n) * row;
-        if (wide) for (long long i = threadIdx.x; i < bytes / 16; i += 256) reinterpret_cast<uint4 *>(at)[i] = make_uint4(0, 0, 0, 0);
-        else for (long long i = threadIdx.x; i < bytes / 2; i += 256) reinterpret_cast<unsigned short *>(at)[i] = 0;
-    }
-}
-
 static DecayArgs common_args(const darkattn_decay_plan_s *plan, const float *log_decay, const int *lengths, int nseg, int cps, int sub, void *ws)
 {
     DecayArgs A = {};
@@ -139,11 +121,7 @@ darkattn_status_t darkattn_decay_backward(darkattn_decay_plan_t plan, const void
     A.pass[1] = DecayPass{V, dO, Q, dK, dS_out, nullptr, R, ds.dv, ds.d, ds.H_kv, ds.H, 1, 1, ds.scale, 1.f, ds.scale, 0};
     A.pass[2] = DecayPass{K, Q, dO, dV, dS_out, dS_in, R, ds.d, ds.dv, ds.H_kv, ds.H, 1, 0, ds.scale, 1.f, ds.scale, dS_in != nullptr};
     DecayPass sets[2] = {{nullptr, K, V, nullptr, S_in, nullptr, S, ds.d, ds.dv, ds.H_kv, ds.H_kv, 0, 0, 0.f, 0.f, 1.f, 0}, A.pass[2]};
-    if (lengths) {
-        const int e = ds.dtype == DARKATTN_BF16 ? 2 : 4;
-        DARKATTN_CUDA_TRY(launch_pdl(decay_zero_tail_kernel, dim3((unsigned)(ds.H < 64 ? ds.H : 64), (unsigned)ds.B, 3), dim3(256), 0, st, static_cast<unsigned char *>(dQ), static_cast<unsigned char *>(dK),
-                                     static_cast<unsigned char *>(dV), lengths, ds.H, ds.H_kv, ds.N, ds.d * e, ds.dv * e), "decay_zero_tail_kernel");
-    }
+    A.zero = lengths != nullptr;
     return run(plan, A, sets, 2, st);
 }
 

@@ -66,6 +66,8 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
     const bool last = sp.T == 0 ? seg == 0 : sp.k0 < sp.k1 && sp.k1 == sp.T;
     float *S_out = MAIN ? (p.S_out && last && hx % (HX / A.Hkv) == 0 ? p.S_out + (size_t)(b * A.Hkv + hs) * a * c : nullptr)
                         : const_cast<float *>(p.seg) + ((size_t)(b * A.Hkv + hs) * nseg + seg) * a * c;
+    T *O = static_cast<T *>(p.O) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * c;
+    if (MAIN && zt == 0) zero_behind<C>(A, sp, seg, O, c, tid, kThreadsS);
     if (sp.k0 == sp.k1 && !(MAIN && last && S_out)) return;
 
     if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
@@ -76,7 +78,6 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
         S[i] = S_in && f < a && z < c ? (p.trans ? S_in[(size_t)z * a + f] : S_in[(size_t)f * c + z]) : 0.f;
     }
     const T *X = static_cast<const T *>(p.X) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * a;
-    T *O = static_cast<T *>(p.O) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * c;
 
     for (int k = sp.k0; k < sp.k1; ++k) {
         const int t0 = (p.reverse ? sp.T - 1 - k : k) * C, L = min(C, sp.n - t0);
@@ -316,6 +317,8 @@ __global__ void __launch_bounds__(kThreadsS) decay_tile_kernel(const __grid_cons
     const size_t state = (size_t)(b * A.Hkv + hs) * a * c;
     float *S_out = MAIN ? (p.S_out && last && hx % (HX / A.Hkv) == 0 ? p.S_out + state : nullptr)
                         : const_cast<float *>(p.seg) + ((size_t)(b * A.Hkv + hs) * nseg + seg) * a * c;
+    T *O = static_cast<T *>(p.O) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * c;
+    if (MAIN) zero_behind<C>(A, sp, seg, O, c, tid, kThreadsS);
     if (sp.k0 == sp.k1 && !(MAIN && last && S_out)) return;
     if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
     const float *S_in = nullptr;
@@ -337,7 +340,6 @@ __global__ void __launch_bounds__(kThreadsS) decay_tile_kernel(const __grid_cons
     };
     if (MAIN) put_state();
     const T *X = static_cast<const T *>(p.X) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * a;
-    T *O = static_cast<T *>(p.O) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * c;
 
     for (int k = sp.k0; k < sp.k1; ++k) {
         const int t0 = (reverse ? sp.T - 1 - k : k) * C, L = min(C, sp.n - t0);

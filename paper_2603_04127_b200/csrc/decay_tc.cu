@@ -284,6 +284,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     }
     __syncthreads();
 
+    if (MAIN && warp != kWarps) zero_behind<C>(A, sp, seg, static_cast<__nv_bfloat16 *>(p.O) + (size_t)head * A.N * c, c, tid < 32 * kWarps ? tid : tid - 32, kBlock - 32);
+
     int *status = A.status;
 
     if (!fine) {
