@@ -118,6 +118,12 @@ inline bool clash(std::initializer_list<Span> out, std::initializer_list<Span> i
     return false;
 }
 
+// Heads whose chunks are one item of work each, and heads that sum over a group of G.
+struct DecayLoad {
+    long long heads, sums;
+    int G;
+};
+
 // FP32 kernels, any shape
 void decay_simt_split(darkattn_decay_plan_s *plan);
 darkattn_status_t decay_simt_run(DecayArgs &A, DecayPass *state_pass, int nstate, int bf16, cudaStream_t st);

@@ -346,6 +346,7 @@ __global__ void __launch_bounds__(kThreadsS) decay_tile_kernel(const __grid_cons
         Row<R> o[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) o[u].clear();
+        const bool mine = warp * 8 < L;                      // the warp has rows (of short chunks few do: 9 tokens of 12 heads on 3, d 128, gradients 67 -> 58 us)
         for (int g = 0; g < G; ++g) {
             const T *Y = static_cast<const T *>(p.Y) + ((size_t)(b * p.HY + hy0 + g) * A.N + t0) * a;
             const T *Z = static_cast<const T *>(p.Z) + ((size_t)(b * p.HY + hy0 + g) * A.N + t0) * c;
@@ -373,8 +374,8 @@ __global__ void __launch_bounds__(kThreadsS) decay_tile_kernel(const __grid_cons
                 Row<4> sc[4];
 #pragma unroll
                 for (int u = 0; u < 4; ++u) sc[u].clear();
-                products<4, 4, 4>(sc, XT, kPad, YT, kPad, a, ty, tx);
-                if (g == 0) {
+                if (mine) products<4, 4, 4>(sc, XT, kPad, YT, kPad, a, ty, tx);
+                if (g == 0 && mine) {
                     products<4, R, R>(o, XT, kPad, Ss, LW, a, ty, tx);
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
@@ -406,7 +407,7 @@ __global__ void __launch_bounds__(kThreadsS) decay_tile_kernel(const __grid_cons
             if (!MAIN) continue;
             __syncthreads();                                 // P is there; the state before this chunk has been read
             // rows 8 warp .. 8 warp + 7 of P: zero behind (backwards: before) the diagonal
-            const int from = reverse ? warp * 8 : 0, to = reverse ? L : min(warp * 8 + 8, L);
+            const int from = reverse ? warp * 8 : 0, to = reverse ? L : mine ? min(warp * 8 + 8, L) : 0;
             products<4, R, R>(o, PT + from * kPad, kPad, Zs + from * LW, LW, to - from, ty, tx);
             if (g == G - 1) put_state();
         }
@@ -542,18 +543,23 @@ darkattn_status_t decay_simt_run(DecayArgs &A, DecayPass *state_pass, int nstate
 
 // Segments: the cheapest by an estimate in units of a chunk's time (fitted to fp32 on a B200: 11 us at width 64 and 22 at 128 by itself, two blocks
 // on an SM 1.35 times that): a chunk of the states alone takes 0.28, three kernels instead of one about one more.
-static void pick(int T, long long units, long long state_units, int per_sm, int &nseg, int &cps, int &sub)
+static void pick(int T, DecayLoad rows, DecayLoad states, int per_sm, int &nseg, int &cps, int &sub)
 {
-    const auto phase = [&](long long blocks, int per, double one) {
+    const auto phase = [&](const DecayLoad &x, long long pieces, int per, double one) {
         const double two = per_sm == 2 ? 1.35 : 1.0;
+        const long long blocks = (x.heads + x.sums) * pieces;
+        if (x.G > 1) {                                       // the heads that sum over a group take longest
+            const double long_one = x.G * (blocks > 148 ? two : 1.0), shared = (double)(x.heads + x.sums * x.G) * pieces / (148 * per_sm) * two;
+            return per * one * (long_one > shared ? long_one : shared);
+        }
         const long long slots = 148LL * per_sm, rest = blocks % slots;
         return per * one * ((double)(blocks / slots) * two + (rest > 148 ? two : rest ? 1.0 : 0.0));
     };
     nseg = 1; cps = T; sub = 1;
-    double best = phase(units, T, 1.0);
+    double best = phase(rows, 1, T, 1.0);
     for (int n = 2; n <= T && n <= 128; ++n) {
         const int per = (T + n - 1) / n, m = (T + per - 1) / per;
-        const double cost = phase(units * m, per, 1.0) + phase(state_units * (m - 1), per, 0.28) + 1.0 + 0.01 * m;
+        const double cost = phase(rows, m, per, 1.0) + phase(states, m - 1, per, 0.28) + 1.0 + 0.01 * m;
         if (cost < best) { best = cost; nseg = m; cps = per; }
     }
 }
@@ -564,8 +570,10 @@ void decay_simt_split(darkattn_decay_plan_s *plan)
     const int T = (ds.N + C - 1) / C, w = ds.d > ds.dv ? ds.d : ds.dv;
     const long long zf = w <= 128 ? 1 : (ds.dv + 63) / 64, zb = w <= 128 ? 1 : (w + 63) / 64;      // tiles of the output's columns
     const int per_sm = w <= 80 ? 2 : 1;
-    pick(T, (long long)ds.B * ds.H * zf, (long long)ds.B * ds.H_kv * zf, per_sm, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub);
-    pick(T, (long long)ds.B * (ds.H + 2 * ds.H) * zb, 2LL * ds.B * ds.H * zf, per_sm, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub);
+    const long long q = (long long)ds.B * ds.H, k = (long long)ds.B * ds.H_kv;
+    const int G = ds.H / ds.H_kv;
+    pick(T, {q * zf, 0, 1}, {k * zf, 0, 1}, per_sm, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub);
+    pick(T, {q * zb, 2 * k * zb, G}, {k * zf, k * zf, G}, per_sm, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub);
 }
 
 }  // namespace darkattn

@@ -8,13 +8,13 @@
 //                                    state; with one, its rounding would show in the rows out.
 // The state itself stays in the registers of eight warps in fp32, S <- lambda^L S + D; the rows read a copy rounded to bf16 (as P is
 // rounded: half a step of each term, like the rounding of the rows out: together 1.4 times the error of that rounding alone).
-// Everything moves by TMA, two chunks of X, Y and Z deep; the rows out are staged in the chunk's own tiles (stored from registers, 32 bytes a
+// Everything moves by TMA, two to four chunks of X, Y and Z deep; the rows out are staged in the chunk's own tiles (stored from registers, 32 bytes a
 // thread, d 128 took 226 us for 212).
 //
 // What bounds it: shared memory. At width 128 a chunk's tiles, operands and copies are 3.8 thousand cycles of its 128 bytes a cycle (the products
 // by themselves 2.6), a chunk takes 4.5 thousand; at 64 2.3 of 3.4 thousand, the rest latencies of steps that wait for one another: scores
 // into P 500, the state 250 to 600, rows out 400, transposition 1100. (Warps of their own for some of the steps, 18 to 28 in all, overlap
-// them and made nothing faster: d 128 219 -> 275 us.) 4 x 37 heads of 8192 tokens, one block an SM: d 128 1.24 GB in 212 us, 5.9 TB/s; d 64 0.62 GB in 130, 4.8.
+// them and made nothing faster: d 128 219 -> 275 us.) 4 x 37 heads of 8192 tokens, one block an SM: d 128 1.24 GB in 215 us, 5.8 TB/s; d 64 0.62 GB in 126, 4.9.
 #include "decay.cuh"
 #include "tc_common.cuh"
 
@@ -654,21 +654,30 @@ cudaError_t launch(const TcArgs &P, cudaStream_t st)
     return launch_pdl(decay_tc_kernel<DY, DZ, MAIN>, dim3((unsigned)blocks), dim3(kBlock), TcSmem<DY, DZ, MAIN>::total, st, P);
 }
 
-// passes whose widths are of one class share a launch
+// Passes whose widths are of one class share a launch. Where one wave of blocks holds them all, every pass does, on wide tiles: a launch waits for
+// the one before (3 x 16 heads on 8 of 1024 tokens, gradients at d 128, dv 64: 82 us in two launches, 65 in one).
 template <bool MAIN>
 darkattn_status_t launch_all(const DecayArgs &A, const DecayPass *pass, int npass, bool first, cudaStream_t st)
 {
     bool done[kDecayPasses] = {};
+    long long blocks = 0;
+    bool y_wide = false, z_wide = false;
+    for (int i = 0; i < npass; ++i) {
+        blocks += (long long)A.B * (MAIN ? pass[i].HX : A.Hkv) * A.nseg;
+        y_wide |= pass[i].a > 64;
+        z_wide |= pass[i].c > 64;
+    }
+    const bool together = blocks <= 148;
     for (int i = 0; i < npass; ++i) {
         if (done[i]) continue;
-        const bool y2 = pass[i].a > 64, z2 = pass[i].c > 64;
+        const bool y2 = together ? y_wide : pass[i].a > 64, z2 = together ? z_wide : pass[i].c > 64;
         TcArgs P;
         P.a = A;
         P.a.clear = first && i == 0;
         int n = 0;
         for (int j = i; j < npass; ++j) {
             const DecayPass &q = pass[j];
-            if (done[j] || (q.a > 64) != y2 || (q.c > 64) != z2) continue;
+            if (done[j] || (!together && ((q.a > 64) != y2 || (q.c > 64) != z2))) continue;
             done[j] = true;
             P.a.pass[n] = q;
             bool ok = make_map3(&P.m[n].y, q.Y, A.B * q.HY, A.N, q.a) && make_map3(&P.m[n].z, q.Z, A.B * q.HY, A.N, q.c);
@@ -697,22 +706,34 @@ bool decay_tc_supported(const darkattn_decay_desc_t &ds)
 // segment, 31 in 32; 4 x 16 heads: 164 in one, 139 in two with two pieces each, 188 in four; 8 heads of 65536, d 64: 113 in 18.
 // Segments have to promise 8 % (a backward pass in one segment shares more of its reads in L2 than the estimate knows: 4 x 16 heads, 337 us
 // in one, 359 in two).
-static void pick(int T, int d, int dv, long long units, long long state_units, int sets, int &nseg, int &cps, int &sub)
+// `heads` heads of a pass take an item a chunk, `sums` of them G: those that sum over a group's heads. Where these are the longer ones nothing is done
+// before they are: 2 x 12 heads on 3, 898 tokens, gradients at d 96, dv 64: 129 us in one segment, 48 in several.
+static void pick(int T, int d, int dv, DecayLoad rows, DecayLoad states, int sets, int &nseg, int &cps, int &sub)
 {
     const bool wide = d > 64 || dv > 64;
     const double chunk = wide ? 2.6 : 1.7, state_chunk = wide ? 1.4 : 1.0, more = sets * (wide ? 9 : 4), rate = wide ? 5.7e6 : 4.8e6;
     const double bytes = 2.0 * C * 2 * (d + dv);
-    const auto phase = [&](long long blocks, int per, double us, double b) {
+    const auto phase = [&](const DecayLoad &x, long long pieces, int per, double us, double b) {
+        const long long blocks = (x.heads + x.sums) * pieces;
         const double all = 148 * b / rate, rest = (double)(blocks % 148) * b / rate;
+        if (x.G > 1) {
+            const double long_one = x.G * us, shared = (double)(x.heads + x.sums * x.G) * pieces / 148 * (all > us ? all : us);
+            return 2.0 * ((blocks + 147) / 148) + per * (long_one > shared ? long_one : shared);
+        }
         return 2.0 * ((blocks + 147) / 148) + per * ((double)(blocks / 148) * (all > us ? all : us) + (blocks % 148 ? (rest > us ? rest : us) : 0));
     };
+    // a backward pass of widths of two classes: dQ and dK by one launch, dV by another, unless one wave holds them
+    const auto main_phase = [&](long long pieces, int per) {
+        if (rows.sums == 0 || (d > 64) == (dv > 64) || (rows.heads + rows.sums) * pieces <= 148) return phase(rows, pieces, per, chunk, bytes);
+        return phase({rows.heads, rows.sums / 2, rows.G}, pieces, per, chunk, bytes) + phase({0, rows.sums / 2, rows.G}, pieces, per, chunk, bytes);
+    };
     nseg = 1; cps = T; sub = 1;
-    double best = phase(units, T, chunk, bytes);
+    double best = main_phase(1, T);
     for (int n = 2; n <= T && n <= 64; ++n) {
         for (int q = 1; q <= 4; ++q) {
             const int per = ((T + n - 1) / n + q - 1) / q * q, m = (T + per - 1) / per;
             if (m < 2) continue;
-            const double cost = 1.08 * (phase(units * m, per, chunk, bytes) + phase(sets * state_units * (m - 1) * q, per / q, state_chunk, bytes / 2) + more + 0.06 * (m - 1) * q);
+            const double cost = 1.08 * (main_phase(m, per) + phase(states, (m - 1) * q, per / q, state_chunk, bytes / 2) + more + 0.06 * (m - 1) * q);
             if (cost < best) { best = cost; nseg = m; cps = per; sub = q; }
         }
     }
@@ -722,8 +743,10 @@ void decay_tc_split(darkattn_decay_plan_s *plan)
 {
     const darkattn_decay_desc_t &ds = plan->desc;
     const int T = (ds.N + C - 1) / C;
-    pick(T, ds.d, ds.dv, (long long)ds.B * ds.H, (long long)ds.B * ds.H_kv, 1, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub);
-    pick(T, ds.d, ds.dv, 3LL * ds.B * ds.H, (long long)ds.B * ds.H, 2, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub);
+    const long long q = (long long)ds.B * ds.H, k = (long long)ds.B * ds.H_kv;
+    const int G = ds.H / ds.H_kv;
+    pick(T, ds.d, ds.dv, {q, 0, 1}, {k, 0, 1}, 1, plan->fwd.nseg, plan->fwd.cps, plan->fwd.sub);
+    pick(T, ds.d, ds.dv, {q, 2 * k, G}, {k, k, G}, 2, plan->bwd.nseg, plan->bwd.cps, plan->bwd.sub);
 }
 
 darkattn_status_t decay_tc_run(DecayArgs &A, DecayPass *state_pass, int nstate, cudaStream_t st)
