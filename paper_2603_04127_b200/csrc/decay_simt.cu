@@ -19,149 +19,6 @@ template <typename T> __device__ __forceinline__ T from_f(float x);
 template <> __device__ __forceinline__ float from_f<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 
-struct SimtSmem {
-    static constexpr int XT = 0, YT = XT + F * kPad, Yr = YT + F * kPad, Z = Yr + C * F, PT = Z + C * F, pw = PT + C * kPad, S = pw + 72;
-    static int bytes(int a) { return (S + (a + F - 1) / F * F * F) * 4; }
-};
-
-// acc += sum over k < 64 of A[k][ty * 4 ..] B[k][tx * 4 ..]
-__device__ __forceinline__ void outer(float (&acc)[4][4], const float *A, int lda, const float *B, int ldb, int ty, int tx)
-{
-#pragma unroll 8
-    for (int k = 0; k < 64; ++k) {
-        const float4 x = *reinterpret_cast<const float4 *>(A + k * lda + ty * 4), y = *reinterpret_cast<const float4 *>(B + k * ldb + tx * 4);
-        const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) acc[u][v] = fmaf(xs[u], ys[v], acc[u][v]);
-    }
-}
-
-// MAIN: rows out; otherwise only the state of each of the first nseg - 1 segments, from zero, into pass.seg
-template <typename T, bool MAIN>
-__global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_constant__ DecayArgs A, int ntz)
-{
-    using M = SimtSmem;
-    extern __shared__ __align__(16) float sm[];
-    float *XT = sm + M::XT, *YT = sm + M::YT, *Yr = sm + M::Yr, *Zs = sm + M::Z, *PT = sm + M::PT, *pw = sm + M::pw, *S = sm + M::S;
-    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-    pdl_wait();
-
-    if (MAIN && blockIdx.x == 0 && tid == 0) *A.status = 0;     // (nothing here waits: the call's status is known)
-    const int nseg = MAIN ? A.nseg : A.nseg - 1;
-    int id = blockIdx.x;
-    const DecayPass &p = A.pass[id % A.npass]; id /= A.npass;
-    const int zt = id % ntz; id /= ntz;
-    const int seg = id % nseg, head = id / nseg;            // head: of X, or of the state
-    const int z0 = zt * F;
-    if (z0 >= p.c) return;
-    const int HX = MAIN ? p.HX : A.Hkv;
-    const int b = head / HX, hx = head % HX;
-    const int hs = hx / (HX / A.Hkv);                        // state and decay
-    const int G = p.HY > HX ? p.HY / HX : 1;                 // heads of Y that are summed over
-    const int hy0 = p.HY > HX ? hx * G : hx / (HX / p.HY);
-    const DecaySpan sp = decay_span<C>(A, b, seg);
-    const int a = p.a, c = p.c, nf = (a + F - 1) / F;
-    const bool last = sp.T == 0 ? seg == 0 : sp.k0 < sp.k1 && sp.k1 == sp.T;
-    float *S_out = MAIN ? (p.S_out && last && hx % (HX / A.Hkv) == 0 ? p.S_out + (size_t)(b * A.Hkv + hs) * a * c : nullptr)
-                        : const_cast<float *>(p.seg) + ((size_t)(b * A.Hkv + hs) * nseg + seg) * a * c;
-    T *O = static_cast<T *>(p.O) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * c;
-    if (MAIN && zt == 0) zero_behind<C>(A, sp, seg, O, c, tid, kThreadsS);
-    if (sp.k0 == sp.k1 && !(MAIN && last && S_out)) return;
-
-    if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
-    const float *S_in = nullptr;
-    if (MAIN) S_in = seg == 0 ? (p.S_in ? p.S_in + (size_t)(b * A.Hkv + hs) * a * c : nullptr) : p.seg + ((size_t)(b * A.Hkv + hs) * (nseg - 1) * A.sub + seg * A.sub - 1) * a * c;
-    for (int i = tid; i < nf * F * F; i += kThreadsS) {
-        const int f = i / F, z = z0 + i % F;
-        S[i] = S_in && f < a && z < c ? (p.trans ? S_in[(size_t)z * a + f] : S_in[(size_t)f * c + z]) : 0.f;
-    }
-    const T *X = static_cast<const T *>(p.X) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * a;
-
-    for (int k = sp.k0; k < sp.k1; ++k) {
-        const int t0 = (p.reverse ? sp.T - 1 - k : k) * C, L = min(C, sp.n - t0);
-        float o[4][4] = {};
-        for (int g = 0; g < G; ++g) {
-            const T *Y = static_cast<const T *>(p.Y) + ((size_t)(b * p.HY + hy0 + g) * A.N + t0) * a;
-            const T *Z = static_cast<const T *>(p.Z) + ((size_t)(b * p.HY + hy0 + g) * A.N + t0) * c;
-            float sc[4][4] = {};
-            __syncthreads();                                 // the tiles of the step before have been read, pw and S are there
-            for (int i = tid; i < C * F; i += kThreadsS) {
-                const int r = i / F, z = z0 + i % F;
-                Zs[i] = r < L && z < c ? to_f(Z[(size_t)r * c + z]) : 0.f;
-            }
-            for (int fs = 0; fs < nf; ++fs) {
-                if (fs) __syncthreads();
-                for (int i = tid; i < C * F; i += kThreadsS) {
-                    const int r = i / F, fl = i % F, f = fs * F + fl;
-                    const bool in = r < L && f < a;
-                    const float y = in ? to_f(Y[(size_t)r * a + f]) : 0.f;
-                    if (MAIN) {
-                        XT[fl * kPad + r] = in ? to_f(X[(size_t)(t0 + r) * a + f]) : 0.f;
-                        YT[fl * kPad + r] = y;
-                    }
-                    Yr[r * F + fl] = in ? y * (pw[p.reverse ? r + 1 : L - 1 - r] * p.tok_mul) : 0.f;
-                }
-                __syncthreads();
-                float d[4][4] = {};
-                if (MAIN) {
-                    outer(sc, XT, kPad, YT, kPad, ty, tx);
-                    if (g == 0) outer(o, XT, kPad, S + fs * F * F, F, ty, tx);
-                }
-                outer(d, Yr, F, Zs, F, ty, tx);
-                if (MAIN && g == 0) __syncthreads();         // the state before this chunk has been read
-                const float keep = g == 0 ? pw[L] : 1.f;
-#pragma unroll
-                for (int u = 0; u < 4; ++u)
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        float &s = S[(fs * F + ty * 4 + u) * F + tx * 4 + v];
-                        s = keep * s + d[u][v];
-                    }
-            }
-            if (!MAIN) continue;
-            if (g == 0) {
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int r = ty * 4 + u;
-                    const float m = r < L ? pw[p.reverse ? L - 1 - r : r + 1] * p.row_mul : 0.f;
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) o[u][v] *= m;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const int n = p.reverse ? tx * 4 + v - (ty * 4 + u) : ty * 4 + u - (tx * 4 + v);
-                    PT[(tx * 4 + v) * kPad + ty * 4 + u] = n >= 0 ? sc[u][v] * (pw[n] * p.p_mul) : 0.f;
-                }
-            __syncthreads();
-            outer(o, PT, kPad, Zs, F, ty, tx);
-        }
-        if (MAIN) {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int r = ty * 4 + u;
-                if (r >= L) continue;
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const int z = z0 + tx * 4 + v;
-                    if (z < c) O[(size_t)(t0 + r) * c + z] = from_f<T>(o[u][v]);
-                }
-            }
-        }
-    }
-    if (S_out) {
-        __syncthreads();
-        for (int i = tid; i < a * F; i += kThreadsS) {
-            const int f = i / F, z = z0 + i % F;
-            if (z < c) S_out[(size_t)f * c + z] = S[i];
-        }
-    }
-}
-
 // ---------------------------------------------------------------- widths up to 128
 // The whole width of X, Y and Z at once: 256 threads, thread (ty, tx) holds R x R numbers of the state in registers (rows of ty, columns of tx)
 // and 4 x R of the rows out. R = 4, 5, 6 or 8 for widths up to 64, 80, 96, 128. Products two numbers at a time (FFMA2: an FFMA was measured
@@ -451,6 +308,155 @@ __global__ void __launch_bounds__(kThreadsS) decay_tile_kernel(const __grid_cons
                 const int f = spot(ty, u, R), z = spot(tx, v, R);
                 if (f < a && z < c) S_out[(size_t)f * c + z] = s[u].get(v);
             }
+    }
+}
+
+// ---------------------------------------------------------------- wider
+// What the tiles above are, by slices of 64 of X and Y and for 64 columns of Z; the scores are formed again for each 64 columns. Bound by the products and
+// the barriers between them: 4 x 16 heads of 2048 tokens, 256 x 256, 2.5 ms (0.9 by their arithmetic alone).
+struct SimtSmem {
+    static constexpr int XT = 0, YT = XT + F * kPad, Yr = YT + F * kPad, Z = Yr + C * F, PT = Z + C * F, pw = PT + C * kPad, S = pw + 72;
+    static int bytes(int a) { return (S + (a + F - 1) / F * F * F) * 4; }
+};
+
+// MAIN: rows out; otherwise only the state of each of the first nseg - 1 segments, from zero, into pass.seg
+template <typename T, bool MAIN>
+__global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_constant__ DecayArgs A, int ntz)
+{
+    using M = SimtSmem;
+    extern __shared__ __align__(16) float sm[];
+    float *XT = sm + M::XT, *YT = sm + M::YT, *Yr = sm + M::Yr, *Zs = sm + M::Z, *PT = sm + M::PT, *pw = sm + M::pw, *S = sm + M::S;
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, warp = tid >> 5, lane = tid & 31, lr = warp * 8 + (lane >> 2), lf = (lane & 3) * 4;
+    pdl_wait();
+
+    if (MAIN && blockIdx.x == 0 && tid == 0) *A.status = 0;     // (nothing here waits: the call's status is known)
+    const int nseg = MAIN ? A.nseg : A.nseg - 1;
+    int id = blockIdx.x;
+    const DecayPass &p = A.pass[id % A.npass]; id /= A.npass;
+    const int zt = id % ntz; id /= ntz;
+    const int seg = id % nseg, head = id / nseg;            // head: of X, or of the state
+    const int z0 = zt * F;
+    if (z0 >= p.c) return;
+    const int HX = MAIN ? p.HX : A.Hkv;
+    const int b = head / HX, hx = head % HX;
+    const int hs = hx / (HX / A.Hkv);                        // state and decay
+    const int G = p.HY > HX ? p.HY / HX : 1;                 // heads of Y that are summed over
+    const int hy0 = p.HY > HX ? hx * G : hx / (HX / p.HY);
+    const DecaySpan sp = decay_span<C>(A, b, seg);
+    const int a = p.a, c = p.c, nf = (a + F - 1) / F;
+    const bool va = a % 4 == 0, vc = c % 4 == 0;
+    const bool last = sp.T == 0 ? seg == 0 : sp.k0 < sp.k1 && sp.k1 == sp.T;
+    float *S_out = MAIN ? (p.S_out && last && hx % (HX / A.Hkv) == 0 ? p.S_out + (size_t)(b * A.Hkv + hs) * a * c : nullptr)
+                        : const_cast<float *>(p.seg) + ((size_t)(b * A.Hkv + hs) * nseg + seg) * a * c;
+    T *O = static_cast<T *>(p.O) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * c;
+    if (MAIN && zt == 0) zero_behind<C>(A, sp, seg, O, c, tid, kThreadsS);
+    if (sp.k0 == sp.k1 && !(MAIN && last && S_out)) return;
+
+    if (tid <= C) pw[tid] = decay_power(A.log_decay[hs], tid);
+    const float *S_in = nullptr;
+    if (MAIN) S_in = seg == 0 ? (p.S_in ? p.S_in + (size_t)(b * A.Hkv + hs) * a * c : nullptr) : p.seg + ((size_t)(b * A.Hkv + hs) * (nseg - 1) * A.sub + seg * A.sub - 1) * a * c;
+    for (int i = tid; i < nf * F * F; i += kThreadsS) {
+        const int f = i / F, z = z0 + i % F;
+        S[i] = S_in && f < a && z < c ? (p.trans ? S_in[(size_t)z * a + f] : S_in[(size_t)f * c + z]) : 0.f;
+    }
+    const T *X = static_cast<const T *>(p.X) + (size_t)(b * p.HX + (MAIN ? hx : 0)) * A.N * a;
+
+    for (int k = sp.k0; k < sp.k1; ++k) {
+        const int t0 = (p.reverse ? sp.T - 1 - k : k) * C, L = min(C, sp.n - t0);
+        const bool mine = warp * 8 < L;                      // the warp has rows
+        Row<4> o[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) o[u].clear();
+        for (int g = 0; g < G; ++g) {
+            const size_t at = (size_t)(b * p.HY + hy0 + g) * A.N + t0 + lr;
+            const T *X1 = X + (size_t)(t0 + lr) * a, *Y = static_cast<const T *>(p.Y) + at * a, *Z = static_cast<const T *>(p.Z) + at * c;
+            Row<4> sc[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) sc[u].clear();
+            for (int fs = 0; fs < nf; ++fs) {
+                float4 lx[4], ly[4], lz[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    lx[j] = ly[j] = lz[j] = make_float4(0, 0, 0, 0);
+                    if (lr < L) {
+                        ly[j] = load4(Y, fs * F + lf + 16 * j, a, va);
+                        if (MAIN) lx[j] = load4(X1, fs * F + lf + 16 * j, a, va);
+                        if (fs == 0) lz[j] = load4(Z, z0 + lf + 16 * j, c, vc);
+                    }
+                }
+                __syncthreads();                             // the tiles of the step before have been read; pw and S are there
+                const float w = lr < L ? pw[p.reverse ? lr + 1 : L - 1 - lr] * p.tok_mul : 0.f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int f = lf + 16 * j;
+                    const float4 x = lx[j], y = ly[j];
+                    if (fs == 0) *reinterpret_cast<float4 *>(Zs + lr * F + f) = lz[j];
+                    if (MAIN) {
+                        XT[f * kPad + lr] = x.x; XT[(f + 1) * kPad + lr] = x.y; XT[(f + 2) * kPad + lr] = x.z; XT[(f + 3) * kPad + lr] = x.w;
+                        YT[f * kPad + lr] = y.x; YT[(f + 1) * kPad + lr] = y.y; YT[(f + 2) * kPad + lr] = y.z; YT[(f + 3) * kPad + lr] = y.w;
+                    }
+                    *reinterpret_cast<float4 *>(Yr + lr * F + f) = make_float4(y.x * w, y.y * w, y.z * w, y.w * w);
+                }
+                __syncthreads();
+                if (MAIN && mine) {
+                    products<4, 4, 4>(sc, XT, kPad, YT, kPad, F, ty, tx);
+                    if (g == 0) products<4, 4, 4>(o, XT, kPad, S + fs * F * F, F, F, ty, tx);
+                }
+                if (k + 1 == sp.k1 && !S_out) continue;      // nobody reads the state behind this chunk
+                Row<4> d[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) d[u].clear();
+                products<4, 4, 4>(d, Yr, F, Zs, F, L, ty, tx);
+                if (MAIN && g == 0) __syncthreads();         // the state before this chunk has been read
+                const float keep = g == 0 ? pw[L] : 1.f;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    float4 *at4 = reinterpret_cast<float4 *>(S + (fs * F + ty * 4 + u) * F + tx * 4);
+                    const float4 s = *at4;
+                    *at4 = make_float4(fmaf(keep, s.x, d[u].get(0)), fmaf(keep, s.y, d[u].get(1)), fmaf(keep, s.z, d[u].get(2)), fmaf(keep, s.w, d[u].get(3)));
+                }
+            }
+            if (!MAIN) continue;
+            if (g == 0) {
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int r = ty * 4 + u;
+                    o[u].scale(r < L ? pw[p.reverse ? L - 1 - r : r + 1] * p.row_mul : 0.f);
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                float x[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int n = p.reverse ? tx * 4 + v - (ty * 4 + u) : ty * 4 + u - (tx * 4 + v);
+                    x[u] = n >= 0 ? sc[u].get(v) * (pw[n] * p.p_mul) : 0.f;
+                }
+                *reinterpret_cast<float4 *>(PT + (tx * 4 + v) * kPad + ty * 4) = make_float4(x[0], x[1], x[2], x[3]);
+            }
+            __syncthreads();
+            const int from = p.reverse ? warp * 8 : 0, to = p.reverse ? L : mine ? min(warp * 8 + 8, L) : 0;
+            products<4, 4, 4>(o, PT + from * kPad, kPad, Zs + from * F, F, to - from, ty, tx);
+        }
+        if (MAIN) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int r = ty * 4 + u;
+                if (r >= L) continue;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const int z = z0 + tx * 4 + v;
+                    if (z < c) O[(size_t)(t0 + r) * c + z] = from_f<T>(o[u].get(v));
+                }
+            }
+        }
+    }
+    if (S_out) {
+        __syncthreads();
+        for (int i = tid; i < a * F; i += kThreadsS) {
+            const int f = i / F, z = z0 + i % F;
+            if (z < c) S_out[(size_t)f * c + z] = S[i];
+        }
     }
 }
 
