@@ -28,6 +28,9 @@ constexpr int C = 128;
 constexpr int kGroups = 2, kWarps = 4 * kGroups, kBlock = 32 * (kWarps + 2);
 constexpr uint32_t kA = 0, kB = 128, kO = 256, kD = 384; // columns of tensor memory
 constexpr uint32_t kX = 320;                             // X S of a narrow Z (64 columns), apart from P Z; of a wide one it goes to kO
+// Chunks of at most kFew rows: P as two bf16 parts, the second where P's columns of tokens 64 .. 95 would be (four steps of K in all instead of eight). Over
+// many rows P's roundings add a root of two to the error of the rows out; a row or two of few heads can come to twice that (0.0030 for 0.0016).
+constexpr int kFew = 32;
 constexpr int kDiag = 68;                                // numbers of each copy of the diagonal blocks' decays
 
 struct TcMaps { CUtensorMap x, y, z, o; };
@@ -373,12 +376,14 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 mma_commit(bars + DS + it % M::kStages);
             }
             if (MAIN) {
+                const bool few = sp.n - first_row(k) <= kFew;
                 ok = wait_tries(bar + 8 * P_READY, it & 1, status);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) mma_ts(tmem + kO, tmem + kA + 8 * q, mndesc(tZ, q), id_z, (DZ == 128 && inter) || g > 0 || q > 0);
+                    for (int q = 0; q < 8; ++q)
+                        if (!few || (q & 3) < 2) mma_ts(tmem + kO, tmem + kA + 8 * q, mndesc(tZ, few ? q & 3 : q), id_z, (DZ == 128 && inter) || g > 0 || q > 0);
                     mma_commit(bars + PZ + it % M::kStages);
                 }
             }
@@ -469,9 +474,9 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         // Blocks of 32 columns of the scores: a warp takes the outer or the inner two (the triangle has as much in either).
         // Off the diagonal by column, and a power for the row, up to the block's near edge; on the diagonal by a table alone.
         const auto block_of = [&](int i) { return cb == 0 ? 3 * i : 1 + i; };
-        float p_row[4 / kGroups];
+        float p_row[2];
 #pragma unroll
-        for (int i = 0; i < 4 / kGroups; ++i) {
+        for (int i = 0; i < 2; ++i) {
             const int blk = block_of(i);
             p_row[i] = (reverse ? blk > quarter : blk < quarter) ? pw[reverse ? blk * 32 - row : row - blk * 32 - 31] : 1.f;
         }
@@ -484,35 +489,56 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             if (MAIN) {                                   // P: the lower (backwards: the upper) triangle, times the decays
                 DWAIT(SCORES, it & 1);
                 tc_fence_after();
-                uint32_t pk[4 / kGroups][16];
+                if (L <= kFew) {
+                    if (cb == 0) {                        // no other warp reads or writes these rows' columns
+                        const bool off = reverse ? 0 > quarter : 0 < quarter;
+                        uint32_t lead[16] = {}, rest[16] = {};
+                        if (off || quarter == 0) {
+                            const float *by = off ? near : diag + (lane & 3) * kDiag + 32 - (lane & ~3);
+                            uint32_t v[32];
+                            tmem_ld32(at + kA, v);
+                            tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 4 / kGroups; ++i) {
-                    const int blk = block_of(i);
-                    const bool off = reverse ? blk > quarter : blk < quarter;
-                    if (off || blk == quarter) {
-                        const float *by = off ? near : diag + (lane & 3) * kDiag + 32 - (lane & ~3);
-                        uint32_t v[32];
-                        tmem_ld32(at + kA + blk * 32, v);
-                        tmem_wait_ld();
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4) {
-                            const float4 w = *reinterpret_cast<const float4 *>(by + j);
-                            float x[4] = {f(v[j]), f(v[j + 1]), f(v[j + 2]), f(v[j + 3])};
-                            mul2(x[0], x[1], p_row[i], p_row[i]);
-                            mul2(x[2], x[3], p_row[i], p_row[i]);
-                            mul2(x[0], x[1], w.x, w.y);
-                            mul2(x[2], x[3], w.z, w.w);
-                            pk[i][j / 2] = pack_bf16(x[0], x[1]);
-                            pk[i][j / 2 + 1] = pack_bf16(x[2], x[3]);
+                            for (int j = 0; j < 32; j += 2) {
+                                float x = f(v[j]) * p_row[0] * by[j], y = f(v[j + 1]) * p_row[0] * by[j + 1];
+                                lead[j / 2] = take_part(x, y);
+                                rest[j / 2] = pack_bf16(x, y);
+                            }
                         }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) pk[i][j] = 0;
+                        tmem_st16(at + kA, lead);
+                        tmem_st16(at + kA + 32, rest);
                     }
-                }
-                quarter_bar<32 * kGroups>(quarter);       // P takes the place of scores that other warps read
+                } else {
+                    uint32_t pk[2][16];
 #pragma unroll
-                for (int i = 0; i < 4 / kGroups; ++i) tmem_st16(at + kA + block_of(i) * 16, pk[i]);
+                    for (int i = 0; i < 2; ++i) {
+                        const int blk = block_of(i);
+                        const bool off = reverse ? blk > quarter : blk < quarter;
+                        if (off || blk == quarter) {
+                            const float *by = off ? near : diag + (lane & 3) * kDiag + 32 - (lane & ~3);
+                            uint32_t v[32];
+                            tmem_ld32(at + kA + blk * 32, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4) {
+                                const float4 w = *reinterpret_cast<const float4 *>(by + j);
+                                float x[4] = {f(v[j]), f(v[j + 1]), f(v[j + 2]), f(v[j + 3])};
+                                mul2(x[0], x[1], p_row[i], p_row[i]);
+                                mul2(x[2], x[3], p_row[i], p_row[i]);
+                                mul2(x[0], x[1], w.x, w.y);
+                                mul2(x[2], x[3], w.z, w.w);
+                                pk[i][j / 2] = pack_bf16(x[0], x[1]);
+                                pk[i][j / 2 + 1] = pack_bf16(x[2], x[3]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) pk[i][j] = 0;
+                        }
+                    }
+                    quarter_bar<32 * kGroups>(quarter);       // P takes the place of scores that other warps read
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) tmem_st16(at + kA + block_of(i) * 16, pk[i]);
+                }
                 if (kBehindScores && whole) {
                     if (rows_y) {
 #pragma unroll

@@ -374,6 +374,28 @@ def test_without_states_and_with_a_scale(binding, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,dv", [(64, 64), (128, 128), (80, 64), (40, 128)])
+def test_few_rows_are_rounded_once(binding, d, dv):
+    """Up to 32 tokens: the scores as two bf16 parts, which leave 2^-16 of each; beside that the rows' own rounding alone."""
+    for N in (1, 2, 3, 17, 31, 32):
+        t = make(3, 4, N, d, dv, 2, "bf16", seed=40 + N, states=False)
+        t["lengths"] = torch.tensor([N, 1, max(N - 1, 0)], dtype=torch.int32)
+        s = 1 / math.sqrt(d)
+        clean, live = blank_padding(t), alive(t)
+        args = [clean[x] for x in ("q", "k", "v", "do")]
+        O, _ = run_forward(binding, poison_padding(dict(t)))
+        n = ops_of(d, dv, N) + 2 ** 7
+        want, _ = oracle_forward(*args[:3], t["g"], s, t["lengths"], None)
+        mag, _ = oracle_forward(*(a.abs() for a in args[:3]), t["g"], s, t["lengths"], None)
+        check(torch.where(live, O.cpu().double(), 0.0), want, mag, n, torch.bfloat16, False, f"{N} O")
+        got = run_backward(binding, poison_padding(dict(t)))
+        want = oracle_backward(*args, t["g"], s, t["lengths"], None, None)
+        mag = oracle_backward(*(a.abs() for a in args), t["g"], s, t["lengths"], None, None)
+        for name, x, w, m in zip(("dQ", "dK", "dV"), got, want, mag):
+            check(x, w, m, 2 * n, torch.bfloat16, False, f"{N} {name}")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_segments_do_not_change_the_result(binding, dtype):
     """One head is cut into segments, the same head among many is not."""
