@@ -374,6 +374,50 @@ def test_without_states_and_with_a_scale(binding, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,shape", [("bf16", (2, 1, 3000, 64, 64, 1)), ("bf16", (2, 2, 2100, 128, 40, 1)), ("bf16", (4, 12, 140, 128, 64, 12)), ("bf16", (4, 16, 140, 64, 96, 4)),
+                                         ("f32", (2, 1, 1700, 63, 65, 1)), ("f32", (2, 2, 1300, 128, 96, 2)), ("f32", (2, 2, 300, 200, 136, 1)), ("bf16", (2, 2, 300, 136, 129, 2))],
+                         ids=str)
+def test_padded_batches_in_segments_and_of_mixed_widths(binding, dtype, shape):
+    """Ends inside, at and before the segments' ends; more than one wave of blocks and widths of two classes; rows of no whole number of 16 bytes."""
+    B, H, N, d, dv, Hk = shape
+    t = make(B, H, N, d, dv, Hk, dtype, seed=70 + N)
+    for lengths in ([N, 0], [N * 3 // 5, 130], [N - 1, 1]):
+        t["lengths"] = torch.tensor([lengths[i % 2] for i in range(B)], dtype=torch.int32)
+        poisoned = poison_padding(dict(t))
+        check_forward(binding, poisoned, tag=f"{lengths} ")
+        check_backward(binding, poisoned, tag=f"{lengths} ")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,dv", [(64, 64), (128, 64), (128, 128)])
+def test_long_sequences_of_many_heads(binding, d, dv):
+    """Many chunks by one block, all stages in use: the same rows as the heads give by themselves, where they are cut into segments."""
+    B, H, N = 2, 80, 4100
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    rnd = lambda *s: torch.randn(*s, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    q, k, v = rnd(B, H, N, d), rnd(B, H, N, d), rnd(B, H, N, dv)
+    g = torch.full((H,), -0.004, device="cuda")
+
+    def forward(q, k, v, g):
+        plan = binding.darkattn_decay_plan(*q.shape, dv=dv)
+        ws = plan.alloc_workspace()
+        O = torch.empty(*v.shape, dtype=q.dtype, device="cuda")
+        binding.darkattn_decay_forward(plan, q, k, v, g, O, ws)
+        assert binding.darkattn_decay_last_device_status(plan, ws) == binding.OK
+        return O, plan.workspace_bytes
+
+    whole, one = forward(q, k, v, g)
+    part, some = forward(q[1:, 77:78].contiguous(), k[1:, 77:78].contiguous(), v[1:, 77:78].contiguous(), g[77:78])
+    assert one == 256 < some
+    # either is off by at most half a step for the rows out, for each score and for the state's copy
+    mag, _ = oracle_forward(*(x[1:, 77:78].float().abs().cpu() for x in (q, k, v)), g[77:78].cpu(), 1 / math.sqrt(d))
+    bound = 2 * (2.0 ** -8 * part.float().abs().cpu() + (2.0 ** -8 + 2.0 ** -16 + ops_of(d, dv, N) * 2.0 ** -23) * mag)
+    assert ((whole[1:, 77:78].double() - part.double()).abs().cpu() <= bound).all()
+    again, _ = forward(q, k, v, g)
+    assert torch.equal(again, whole)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d,dv", [(64, 64), (128, 128), (80, 64), (40, 128)])
 def test_few_rows_are_rounded_once(binding, d, dv):
     """Up to 32 tokens: the scores as two bf16 parts, which leave 2^-16 of each; beside that the rows' own rounding alone."""
