@@ -149,8 +149,9 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *at, float a, float b, floa
     *reinterpret_cast<uint2 *>(at) = make_uint2(*reinterpret_cast<const unsigned *>(&x), *reinterpret_cast<const unsigned *>(&y));
 }
 
+// (Up to 80 columns two blocks fit an SM's shared memory, and have to fit its registers: with one, 4 x 24 heads of 2000 tokens, d 80, 422 us for 348.)
 template <typename T, int R, bool MAIN>
-__global__ void __launch_bounds__(kThreadsS) decay_tile_kernel(const __grid_constant__ DecayArgs A)
+__global__ void __launch_bounds__(kThreadsS, R <= 5 ? 2 : 1) decay_tile_kernel(const __grid_constant__ DecayArgs A)
 {
     using M = TileSmem<R>;
     constexpr int LW = M::LW;
@@ -219,6 +220,8 @@ __global__ void __launch_bounds__(kThreadsS) decay_tile_kernel(const __grid_cons
         }
     };
 
+    // X S is left out where the state is zero: before a first chunk (12 heads of 100 tokens, d 128: 35.5 -> 29.8 us). Not where two blocks share an SM and
+    // others of the grid do have a state: 2 x 12 heads of 1000 tokens, d 80, in 16 segments took 56 us for 51.
     for (int k = sp.k0; k < sp.k1; ++k) {
         const int t0 = (reverse ? sp.T - 1 - k : k) * C, L = min(C, sp.n - t0);
         Row<R> o[4];
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__(kThreadsS) decay_tile_kernel(const __grid_cons
 #pragma unroll
                 for (int u = 0; u < 4; ++u) sc[u].clear();
                 if (mine) products<4, 4, 4>(sc, XT, kPad, YT, kPad, a, ty, tx);
-                if (g == 0 && mine) {
+                if (g == 0 && mine && (S_in || k > sp.k0 || (R <= 5 && nseg > 1))) {
                     products<4, R, R>(o, XT, kPad, Ss, LW, a, ty, tx);
 #pragma unroll
                     for (int u = 0; u < 4; ++u) {
@@ -400,7 +403,7 @@ __global__ void __launch_bounds__(kThreadsS) decay_simt_kernel(const __grid_cons
                 __syncthreads();
                 if (MAIN && mine) {
                     products<4, 4, 4>(sc, XT, kPad, YT, kPad, F, ty, tx);
-                    if (g == 0) products<4, 4, 4>(o, XT, kPad, S + fs * F * F, F, F, ty, tx);
+                    if (g == 0 && (S_in || k > sp.k0)) products<4, 4, 4>(o, XT, kPad, S + fs * F * F, F, F, ty, tx);
                 }
                 if (k + 1 == sp.k1 && !S_out) continue;      // nobody reads the state behind this chunk
                 Row<4> d[4];
@@ -498,12 +501,9 @@ cudaError_t launch_tile(const DecayArgs &A, cudaStream_t st)
     int heads = 0;
     for (int i = 0; i < A.npass; ++i) heads = max(heads, MAIN ? A.B * A.pass[i].HX : A.B * A.Hkv);
     const long long blocks = (long long)A.npass * (MAIN ? A.nseg : A.nseg - 1) * heads;
-    // Few blocks by an ordinary launch: such as start early, while the kernel before is still on some of the SMs, go two to an SM on the others
-    // (24 heads of 1000 tokens, d 80, in four segments: 127 us, by an ordinary launch 90; in 16 segments 63.5 and 66).
-    if (blocks > 148) return launch_pdl(decay_tile_kernel<T, R, MAIN>, dim3((unsigned)blocks), dim3(kThreadsS), TileSmem<R>::total, st, A);
-    if (cudaError_t e = allow_smem(reinterpret_cast<const void *>(decay_tile_kernel<T, R, MAIN>), TileSmem<R>::total)) return e;
-    decay_tile_kernel<T, R, MAIN><<<dim3((unsigned)blocks), dim3(kThreadsS), TileSmem<R>::total, st>>>(A);
-    return cudaGetLastError();
+    // (Ordinary launches up to 148 blocks, so that none start early and go two to an SM: 12 heads of 700 tokens, d 64, 22.9 us for 19.4; at best 2 and 4 %
+    // less, 128 and 140 heads in one segment.)
+    return launch_pdl(decay_tile_kernel<T, R, MAIN>, dim3((unsigned)blocks), dim3(kThreadsS), TileSmem<R>::total, st, A);
 }
 
 template <typename T, bool MAIN>
@@ -561,8 +561,8 @@ darkattn_status_t decay_simt_run(DecayArgs &A, DecayPass *state_pass, int nstate
     return DARKATTN_OK;
 }
 
-// Segments: the cheapest by an estimate in units of a chunk's time (fitted to fp32 on a B200: 11 us at width 64 and 22 at 128 by itself, two blocks
-// on an SM 1.35 times that): a chunk of the states alone takes 0.28, three kernels instead of one about one more.
+// Segments: the cheapest by an estimate in units of the time of a chunk by itself, fitted to fp32 on a B200: two blocks on an SM take 1.35 times as long, a
+// chunk of the states alone 0.28, three kernels instead of one about one more.
 static void pick(int T, DecayLoad rows, DecayLoad states, int per_sm, int &nseg, int &cps, int &sub)
 {
     const auto phase = [&](const DecayLoad &x, long long pieces, int per, double one) {
