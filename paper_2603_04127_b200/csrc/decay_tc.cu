@@ -39,7 +39,7 @@ struct TcArgs { DecayArgs a; TcMaps m[kDecayPasses]; };
 constexpr int kMostStages = 4;
 // A wait sees one bit of a barrier's count, so nobody may be two phases behind. The products and the warps between them wait for one another item by
 // item; the warp that loads and stores does not hold them up until they need a stage from it, so what it waits for has a barrier for each stage.
-enum { FULL, DS = FULL + kMostStages, PZ = DS + kMostStages, SCORES = PZ + kMostStages, INTER, TMA_BARS, P_READY = TMA_BARS, T_READY, S_READY, O_READ, CLEAN, STAGED, NBARS = STAGED + kMostStages };
+enum { FULL, DS = FULL + kMostStages, PZ = DS + kMostStages, SCORES = PZ + kMostStages, INTER, TMA_BARS, P_READY = TMA_BARS, T_READY, THIRD_READY, S_READY, O_READ, CLEAN, STAGED, NBARS = STAGED + kMostStages };
 
 template <int DY, int DZ, bool MAIN>
 struct TcSmem {
@@ -246,6 +246,9 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     const bool has0 = MAIN && S_in != nullptr;
     const int kept = MAIN && !S_out ? nchunk - 1 : nchunk;      // chunks behind which somebody reads the state
     const bool whole = MAIN ? S_out != nullptr : p.whole;   // three parts
+    // A third part that follows the scores, its product behind P Z (d 128, 8 x 16 heads on 4 of 2001 tokens with states: all three
+    // parts' product behind the scores, before P Z, 78 us, so 74).
+    const bool later = kBehindScores && whole;
     // The states alone are summed from a piece's last chunk to its first (by the power of the decay to the piece's end): the pass that follows starts
     // where this one ends, on what is then in L2.
     const auto first_row = [&](int k) {
@@ -304,6 +307,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         for (int it = 0, k = 0, g = 0; it < items && ok; ++it) {
             const int next = it + M::kStages;
             ok = wait_tries(bar + 8 * ((MAIN ? PZ : DS) + it % M::kStages), it / M::kStages & 1, status);
+            if (ok && later) ok = wait_tries(bar + 8 * (DS + it % M::kStages), it / M::kStages & 1, status);      // the last to read Y and Z
             if (!ok) break;
             if ((M::kEarly || !MAIN) && next < items) load_yz(next, k1, g1);
             if (MAIN && g == G - 1) {
@@ -328,7 +332,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         // In this order the pipe has something to do while the warps turn scores into P (X S, D), scale X S (D) and take the state (P Z).
         const uint32_t id_scores = make_idesc(128, 128, 0, 0), id_z = make_idesc(128, DZ, 0, 1), id_d = kHalves ? make_idesc(128, 128, 0, 1) : id_z;
         const TileDesc tS(sS);
-        const int parts = whole ? 3 : 2;
+        const int parts = whole && !later ? 3 : 2;
         bool ok = true;
         int clean = 0;
         for (int it = 0, k = 0, g = 0; it < items && ok; ++it, k += g + 1 == G, g = g + 1 == G ? 0 : g + 1) {
@@ -373,7 +377,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     for (int q = 0; q < (kHalves ? 4 : 8); ++q)
                         mma_ts(tmem + kD, left + 8 * q, kHalves ? halves + (uint64_t)(q * 2048 >> 4) : mndesc(tZ, q), id_d, g > 0 || part > 0 || q > 0);
                 }
-                mma_commit(bars + DS + it % M::kStages);
+                if (!later) mma_commit(bars + DS + it % M::kStages);
             }
             if (MAIN) {
                 const bool few = sp.n - first_row(k) <= kFew;
@@ -385,6 +389,16 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     for (int q = 0; q < 8; ++q)
                         if (!few || (q & 3) < 2) mma_ts(tmem + kO, tmem + kA + 8 * q, mndesc(tZ, few ? q & 3 : q), id_z, (DZ == 128 && inter) || g > 0 || q > 0);
                     mma_commit(bars + PZ + it % M::kStages);
+                }
+                if (later) {
+                    ok = wait_tries(bar + 8 * THIRD_READY, it & 1, status);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) mma_ts(tmem + kD, tmem + kThird + 8 * q, mndesc(tZ, q), id_d, true);
+                        mma_commit(bars + DS + it % M::kStages);
+                    }
                 }
             }
         }
@@ -465,7 +479,6 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     else weighted_transpose<kBehindScores ? LEAD : ALL, kPart>(stage + y_own + t * 4096, w, at + kB + t * 16, at + kThird + t * 16);
                 }
             }
-            if (kBehindScores && whole) return;           // the third part follows when the scores have been read
             tmem_wait_st();
             tc_fence_before();
             arrive_warp(bar + 8 * T_READY, lane);
@@ -539,18 +552,6 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
 #pragma unroll
                     for (int i = 0; i < 2; ++i) tmem_st16(at + kA + block_of(i) * 16, pk[i]);
                 }
-                if (kBehindScores && whole) {
-                    if (rows_y) {
-#pragma unroll
-                        for (int tb = 0; tb < 4 / kGroups; ++tb) {
-                            const int t = cb + kGroups * tb;
-                            weighted_transpose<THIRD, kPart>(sbase + it % M::kStages * M::kStage + y_own + t * 4096, tok + t * 32 + 2 * (lane & 3), 0, at + kThird + t * 16);
-                        }
-                    }
-                    tmem_wait_st();
-                    tc_fence_before();
-                    arrive_warp(bar + 8 * T_READY, lane);
-                }
                 if (L != Lx) {
                     x_row = row < L ? row_mul * pw[reverse ? L - 1 - row : row + 1] : 0.f;
                     Lx = L;
@@ -571,6 +572,18 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 tmem_wait_st();
                 tc_fence_before();
                 arrive_warp(bar + 8 * P_READY, lane);
+                if (later) {
+                    if (rows_y) {
+#pragma unroll
+                        for (int tb = 0; tb < 4 / kGroups; ++tb) {
+                            const int t = cb + kGroups * tb;
+                            weighted_transpose<THIRD, kPart>(sbase + it % M::kStages * M::kStage + y_own + t * 4096, tok + t * 32 + 2 * (lane & 3), 0, at + kThird + t * 16);
+                        }
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    arrive_warp(bar + 8 * THIRD_READY, lane);
+                }
             }
             if (k < kept) DWAIT(DS + it % M::kStages, it / M::kStages & 1);
             if (k < kept && g == G - 1) {
