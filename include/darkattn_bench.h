@@ -21,6 +21,10 @@ int32_t darkattn_plan_launches(darkattn_plan_t plan, int32_t which);
  * up the others. 0 without the mask and on the FP32 path.                                          */
 double darkattn_plan_rows_summed(darkattn_plan_t plan);
 
+/* How a call of attention with a decay per head is cut: split (HOST array of 3) receives the segments of a sequence of N tokens, the chunks
+ * of each, and the pieces that each of the first ones is cut into where their states are summed. which: 0 forward, 1 backward. */
+darkattn_status_t darkattn_decay_plan_split(darkattn_decay_plan_t plan, int32_t which, int32_t *split);
+
 /* Per-kernel device times, for benchmarks. While enabled, forward and backward record a CUDA event on
  * the call's stream in front of every kernel they launch and one behind the last (events are host
  * objects created by the first enabling call; no device memory is involved). Enabling also clears the

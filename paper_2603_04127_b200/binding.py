@@ -31,7 +31,8 @@ EXPORTS = [
     "darkattn_state_store", "darkattn_state_load",
 ]
 # instruments of the benchmark, in a library of their own (include/darkattn_bench.h)
-BENCH_EXPORTS = ["darkattn_plan_launches", "darkattn_plan_rows_summed", "darkattn_kernel_timing", "darkattn_kernel_times", "darkattn_measure_mma_cycles"]
+BENCH_EXPORTS = ["darkattn_plan_launches", "darkattn_plan_rows_summed", "darkattn_decay_plan_split", "darkattn_kernel_timing", "darkattn_kernel_times",
+                 "darkattn_measure_mma_cycles"]
 STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -124,6 +125,8 @@ def benchlib():
         b.darkattn_plan_launches.restype = ctypes.c_int32
         b.darkattn_plan_rows_summed.argtypes = [_vp]
         b.darkattn_plan_rows_summed.restype = ctypes.c_double
+        b.darkattn_decay_plan_split.argtypes = [_vp, ctypes.c_int32, ctypes.POINTER(ctypes.c_int32)]
+        b.darkattn_decay_plan_split.restype = ctypes.c_int
         b.darkattn_measure_mma_cycles.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_double),
                                                   ctypes.POINTER(ctypes.c_double), _vp]
         b.darkattn_measure_mma_cycles.restype = ctypes.c_int
@@ -332,6 +335,12 @@ class DecayPlan:
     @property
     def path(self) -> int:
         return int(lib.darkattn_decay_plan_path(self.handle))
+
+    def split(self, backward: bool = False):
+        """(segments of a sequence, chunks of each, pieces of each where states are summed)"""
+        cut = (ctypes.c_int32 * 3)()
+        _check(benchlib().darkattn_decay_plan_split(self.handle, 1 if backward else 0, cut), "darkattn_decay_plan_split")
+        return tuple(cut)
 
     def alloc_workspace(self, device="cuda") -> torch.Tensor:
         return torch.empty(self.workspace_bytes, dtype=torch.uint8, device=device)

@@ -1,7 +1,7 @@
 // Instruments of the benchmark and of the profiling runs, kept out of the product library: per-kernel device times
 // (the product's launch code records events at every kernel while a plan's timer is on; these calls switch it on and
 // harvest it) and the number of launches of a call. Built into libdarkattn_bench.so, which links against libdarkattn.so.
-#include "../csrc/common.cuh"
+#include "../csrc/decay.cuh"
 #include "darkattn_bench.h"
 
 #include <stdio.h>
@@ -29,6 +29,14 @@ double darkattn_plan_rows_summed(darkattn_plan_t plan)
         chunks += len < Y.cut ? len : Y.cut;
     }
     return (double)chunks / Y.T;
+}
+
+darkattn_status_t darkattn_decay_plan_split(darkattn_decay_plan_t plan, int32_t which, int32_t *split)
+{
+    if (!plan || !split) return DARKATTN_ERR_INVALID_ARG;
+    const auto &cut = which ? plan->bwd : plan->fwd;
+    split[0] = cut.nseg; split[1] = cut.cps; split[2] = cut.sub;
+    return DARKATTN_OK;
 }
 
 darkattn_status_t darkattn_kernel_timing(darkattn_plan_t plan, int32_t enable)
