@@ -1,6 +1,5 @@
 """Attention with a decay per head where a sequence is cut into segments of several chunks, and these into pieces: the cut that long prompts and
-training
-steps have, against the quadratic form in 64 bits.
+training steps have. With and without the optional states, against the quadratic form in 64 bits.
 
 Bounds. FP32 arithmetic: `check` of test_decay.py, element by element. bf16 rows: beside that, which grows with the number of terms where errors of
 either sign grow like its root, two on the norm of the error, for every head by itself.
@@ -239,8 +238,13 @@ def _cases():
     out = []
     for shape, *_ in CUT:
         N = shape[2]
-        for lengths in (None, [N * 7 // 10 + 1, N - 200], [N // 2, 130]):
-            out.append((shape, lengths, ("S", "dS"), True))
+        # states: all four; none; those in without the one out, one of them in, and the other way round
+        out.append((shape, None, ("S", "dS"), True))
+        out.append((shape, None, (), False))
+        out.append((shape, None, ("S", "dS"), False))
+        out.append((shape, [N * 7 // 10 + 1, N - 200], ("dS",), False))
+        out.append((shape, [N // 2, 130], (), True))
+        out.append((shape, [N - 1, N // 3], ("S",), True))
     return out
 
 
