@@ -202,18 +202,25 @@ CUT = [
     ((2, 8, 2000, 200, 136, 8, "f32", 0), (True, False), (True, False)),
     ((1, 16, 3000, 256, 256, 4, "bf16", 0), (True, False), (False, False)),
     ((2, 12, 1500, 96, 64, 3, "bf16", 1), None, None),
+    # one segment, many chunks by one block, all stages in use
+    ((2, 50, 2100, 64, 64, 50, "bf16", 0), None, None),
+    ((2, 75, 1500, 128, 64, 75, "bf16", 0), None, None),
+    ((2, 75, 1500, 64, 128, 75, "bf16", 0), None, None),
+    ((2, 75, 1500, 128, 128, 75, "bf16", 0), None, None),
 ]
 
 
 @pytest.mark.parametrize("shape,forward,backward", CUT, ids=str)
 def test_the_cuts_are_what_these_tests_are_about(binding, shape, forward, backward):  # noqa: F811
     """(Refitting the estimate that cuts sequences may change these: then other shapes have to take their places.)"""
-    plan = _plan(binding, *shape)
+    plan, path = _plan(binding, *shape), shape[-1]
     for which, want in ((False, forward), (True, backward)):
         if want is not None:
             nseg, cps, sub = plan.split(which)
             assert nseg > 1 and (cps > 1, sub > 1) == want, (which, nseg, cps, sub)
             assert cps % sub == 0
+        elif path == 0:
+            assert plan.split(which)[0] == 1 or forward is not None
     plan.destroy()
 
 
@@ -236,15 +243,17 @@ def _inputs(shape, seed, states_in, lengths):
 
 def _cases():
     out = []
-    for shape, *_ in CUT:
+    for shape, forward, _ in CUT:
         N = shape[2]
         # states: all four; none; those in without the one out, one of them in, and the other way round
-        out.append((shape, None, ("S", "dS"), True))
         out.append((shape, None, (), False))
+        out.append((shape, [N - 1, N // 3], ("S",), True))
+        if forward is None:
+            continue
+        out.append((shape, None, ("S", "dS"), True))
         out.append((shape, None, ("S", "dS"), False))
         out.append((shape, [N * 7 // 10 + 1, N - 200], ("dS",), False))
         out.append((shape, [N // 2, 130], (), True))
-        out.append((shape, [N - 1, N // 3], ("S",), True))
     return out
 
 
