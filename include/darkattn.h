@@ -176,10 +176,10 @@ const char *darkattn_last_cuda_error(void);
 darkattn_status_t darkattn_measure_alu_peak(int32_t which, int32_t iters, double *ops_per_second,
                                             void *cuda_stream);
 
-/* Self-test of the bounded device-side wait the scan kernels rely on: launches one small kernel whose
- * only thread waits on a barrier nobody arrives on. The wait must give up after its limit (2 s),
+/* Self-test of the bounded device-side waits the tensor kernels rely on: launches one small kernel whose
+ * two blocks wait on a barrier nobody arrives on, by the clock or by a number of tries. Each must give up after its limit (2 s),
  * record DARKATTN_ERR_TIMEOUT in a device status word and let the kernel end normally. Writes that
- * status word and the kernel's device time in seconds to the two host pointers; synchronises the
+ * status (-1 where the two differ) and the kernel's device time in seconds to the two host pointers; synchronises the
  * stream. Nothing faults, the context stays usable. Returns DARKATTN_OK when the launch itself ran. */
 darkattn_status_t darkattn_selftest_wait_limit(int32_t *device_status, double *seconds, void *cuda_stream);
 

@@ -69,21 +69,6 @@ template <int N> __device__ __forceinline__ void tmem_ld(uint32_t a, uint32_t (&
 __device__ __forceinline__ float f(uint32_t x) { return __uint_as_float(x); }
 
 // Shared memory by its 32-bit addresses: all of a block's are one number, read once, and constants.
-// A wait with a limit on the number of tries; one answer for the warp. A try that finds nothing suspends the warp until the barrier's phase ends, 4 us
-// at most (measured), so that half a million are the 2 s of tc::warp_wait, whose timer and flag cost a block of 64-column tiles a tenth of its time.
-__device__ __forceinline__ bool wait_tries(uint32_t bar, uint32_t parity, int *status)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 500000;\n\t"
-        "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
-        "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n\t"
-        "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    if (__all_sync(0xffffffffu, ok)) return true;
-    atomicExch(status, 5 /* DARKATTN_ERR_TIMEOUT */);
-    return false;
-}
 __device__ __forceinline__ void arrive_warp(uint32_t bar, int lane)
 {
     __syncwarp();
@@ -306,12 +291,12 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             if (++g1 == G) { g1 = 0; ++k1; }
         for (int it = 0, k = 0, g = 0; it < items && ok; ++it) {
             const int next = it + M::kStages;
-            ok = wait_tries(bar + 8 * ((MAIN ? PZ : DS) + it % M::kStages), it / M::kStages & 1, status);
-            if (ok && later) ok = wait_tries(bar + 8 * (DS + it % M::kStages), it / M::kStages & 1, status);      // the last to read Y and Z
+            ok = warp_wait_tries(bar + 8 * ((MAIN ? PZ : DS) + it % M::kStages), it / M::kStages & 1, status);
+            if (ok && later) ok = warp_wait_tries(bar + 8 * (DS + it % M::kStages), it / M::kStages & 1, status);      // the last to read Y and Z
             if (!ok) break;
             if ((M::kEarly || !MAIN) && next < items) load_yz(next, k1, g1);
             if (MAIN && g == G - 1) {
-                ok = wait_tries(bar + 8 * (STAGED + k % M::kStages), k / M::kStages & 1, status);
+                ok = warp_wait_tries(bar + 8 * (STAGED + k % M::kStages), k / M::kStages & 1, status);
                 if (!ok) break;
                 if (sp.n - first_row(k) >= C && elect_one()) {
                     for (int x = 0; x < DZ && x < c; x += 64) tma_store_3d(&m.o, stage_of(it) + x * 256, x, first_row(k), head);
@@ -340,8 +325,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             const TileDesc tX(stage), tY(stage + M::kX), tZ(stage + M::kX + M::kY);
             const bool inter = has0 || k > 0;
             if (MAIN) {
-                ok = wait_tries(bar + 8 * (FULL + it % M::kStages), it / M::kStages & 1, status);
-                if (ok && sp.n - first_row(k) < C) ok = wait_tries(bar + 8 * CLEAN, clean++ & 1, status);
+                ok = warp_wait_tries(bar + 8 * (FULL + it % M::kStages), it / M::kStages & 1, status);
+                if (ok && sp.n - first_row(k) < C) ok = warp_wait_tries(bar + 8 * CLEAN, clean++ & 1, status);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
@@ -351,8 +336,8 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 }
             }
             if (g == 0) {
-                ok = wait_tries(bar + 8 * S_READY, k & 1, status);
-                if (MAIN && ok && k > 0) ok = wait_tries(bar + 8 * O_READ, (k - 1) & 1, status);
+                ok = warp_wait_tries(bar + 8 * S_READY, k & 1, status);
+                if (MAIN && ok && k > 0) ok = warp_wait_tries(bar + 8 * O_READ, (k - 1) & 1, status);
                 if (!ok) break;
                 if (MAIN && inter) {
                     tc_fence_after();
@@ -365,7 +350,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 }
             }
             if (k < kept) {
-                ok = wait_tries(bar + 8 * T_READY, it & 1, status);
+                ok = warp_wait_tries(bar + 8 * T_READY, it & 1, status);
                 if (!ok) break;
                 tc_fence_after();
             }
@@ -381,7 +366,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
             }
             if (MAIN) {
                 const bool few = sp.n - first_row(k) <= kFew;
-                ok = wait_tries(bar + 8 * P_READY, it & 1, status);
+                ok = warp_wait_tries(bar + 8 * P_READY, it & 1, status);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
@@ -391,7 +376,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                     mma_commit(bars + PZ + it % M::kStages);
                 }
                 if (later) {
-                    ok = wait_tries(bar + 8 * THIRD_READY, it & 1, status);
+                    ok = warp_wait_tries(bar + 8 * THIRD_READY, it & 1, status);
                     if (!ok) break;
                     tc_fence_after();
                     if (elect_one()) {
@@ -439,7 +424,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
         arrive_warp(bar + 8 * S_READY, lane);
         // A wait that gave up ends all further waiting, not the loop: the warps still meet at their barriers, on numbers that mean nothing.
         bool ok = true;
-#define DWAIT(b, ph) do { if (ok) ok = wait_tries(bar + 8 * (b), (ph), status); } while (0)
+#define DWAIT(b, ph) do { if (ok) ok = warp_wait_tries(bar + 8 * (b), (ph), status); } while (0)
         int Ltok = -1;
         uint32_t inters = 0;
         // Brings item `it`'s weighted Y (of a chunk of L rows) into tensor memory.

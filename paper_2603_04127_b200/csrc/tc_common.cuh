@@ -306,6 +306,25 @@ __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, int *s
 {
     return __all_sync(0xffffffffu, wait_or_abort(bar, parity, status, abort_flag));
 }
+// The same on a barrier's 32-bit shared address with a limit on the number of tries, for the decay kernel's loops. A try that finds nothing suspends
+// the warp until the barrier's phase ends, 4 us at most as measured on a B200, so that half a million are the 2 s of warp_wait (the self-test holds it
+// to that). Would tries not suspend at all, they were milliseconds still, where the longest healthy wait, for a block's own loads and products, is
+// some tens of microseconds. A look at the timer costs more than it would tell, even behind the last try: as warp_wait's loop a tenth of the time of blocks
+// of 64-column tiles, as a call behind the first 500 tries 2 to 4 %, as instructions there 0.5 to 4 (registers). The flag is not looked at: who waits for a
+// thread that gave up runs out of tries by itself.
+__device__ __forceinline__ bool warp_wait_tries(uint32_t bar, uint32_t parity, int *status)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, 500000;\n\t"
+        "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
+        "sub.u32 n, n, 1;\n\tsetp.ne.u32 q, n, 0;\n\t@q bra TRY;\n\t"
+        "DONE:\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    if (__all_sync(0xffffffffu, ok)) return true;
+    atomicExch(status, 5 /* DARKATTN_ERR_TIMEOUT */);
+    return false;
+}
 
 // ---------------------------------------------------------------- tiles, epilogue layout, descriptors
 __device__ __forceinline__ unsigned char *tile_chunk(unsigned char *base, int row, int chunk16)

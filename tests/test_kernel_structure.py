@@ -70,3 +70,45 @@ def test_a_wait_has_one_answer_before_tensor_memory_is_read(file, name, body):
         if access:
             between = body[wait.end():wait.end() + access.start()]
             assert "__all_sync(" in between or "warp_wait(" in between, f"{file}: {name}: {body[wait.start():wait.start() + 60]}"
+
+
+def _functions(src):
+    """(name, body) of every function of a source without comments."""
+    for m in re.finditer(r"(\w+)\s*\([^;{}()]*(?:\([^;{}()]*\)[^;{}()]*)*\)\s*\{", src):
+        depth, i = 0, m.end() - 1
+        while True:
+            depth += {"{": 1, "}": -1}.get(src[i], 0)
+            if depth == 0:
+                break
+            i += 1
+        yield m.group(1), src[m.end() - 1:i + 1]
+
+
+def _sources():
+    for path in sorted(glob.glob(os.path.join(CSRC, "*.cu*"))):
+        with open(path) as f:
+            yield os.path.basename(path), re.sub(r"//[^\n]*|/\*.*?\*/", "", f.read(), flags=re.S)
+
+
+def test_every_loop_over_tries_is_limited_and_in_the_self_test():
+    """A loop over tries of a barrier ends by the clock or by their number; the self-test lets it run out, by itself or in a wait made of it."""
+    bodies = {name: body for _, src in _sources() for name, body in _functions(src)}
+    loops = {name for name, body in bodies.items() if re.search(r"\bmbar_try_wait\(", body) and re.search(r"\b(?:for|while)\b", body)}
+    loops |= {name for name, body in bodies.items() if "mbarrier.try_wait" in body and re.search(r"\bbra\b|\bfor\b|\bwhile\b", body)}
+    assert loops == {"mbar_wait_limited", "warp_wait_tries"}
+    assert "kWaitLimitNs" in bodies["mbar_wait_limited"]
+    assert re.search(r"mov\.u32 n, \d+;.*sub\.u32 n, n, 1;.*setp\.ne\.u32 q, n, 0;.*@q bra", bodies["warp_wait_tries"], re.S)
+    assert "mbar_wait_limited(" in bodies["wait_or_abort"]
+    selftest = dict(_sources())["selftest.cu"]
+    assert "warp_wait_tries(" in selftest and "wait_or_abort(" in selftest
+
+
+@pytest.mark.parametrize("file,name,body", TENSOR_MEMORY, ids=[k[1] for k in TENSOR_MEMORY])
+def test_the_waits_of_tensor_memory_kernels_are_known(file, name, body):
+    """Those that a lane answers by itself are looked at above; the others vote."""
+    waits = set(re.findall(r"\b(\w*wait\w*)\(", body)) - {"pdl_wait_tma", "tmem_wait_ld", "tmem_wait_st", "tma_store_wait_read", "tma_store_wait_all"}
+    waits -= set(re.findall(r"auto (\w+) = \[&\]", body))         # made of the others
+    voting = {"warp_wait", "warp_wait_tries"}
+    assert waits and waits <= voting | {"wait_or_abort", "mbar_wait"}, f"{file}: {name}: {waits}"
+    common = dict(_functions(dict(_sources())["tc_common.cuh"]))
+    assert all("__all_sync(" in common[w] for w in voting)
