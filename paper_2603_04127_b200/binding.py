@@ -440,31 +440,36 @@ def darkattn_decay_last_device_status(plan: DecayPlan, workspace, stream=None) -
     return int(lib.darkattn_decay_last_device_status(plan.handle, _ptr(workspace), _stream(stream)))
 
 
-def _state_args(S, codes, scales, slots, dev):
-    """(B, rows, cols) and n_slots, after the checks; the addresses are the caller's to take."""
+# what may hold the codes of a format: their own type, or plain bytes
+_CODES = {STATE_I8: (torch.int8, torch.uint8), STATE_E4M3: (torch.float8_e4m3fn, torch.uint8)}
+
+
+def _state_args(S, codes, scales, slots, format):
+    """The device, (B, rows, cols) and n_slots, after the checks; the addresses."""
     shape, kept = S.shape, codes.shape
     if len(shape) < 2 or len(kept) != len(shape) or codes.element_size() != 1:
         raise ValueError("S is [B, ..., cols], codes one byte an element [n_slots, ..., cols]")
+    if codes.dtype not in _CODES.get(format, (codes.dtype,)):        # (an unknown format is the library's to refuse)
+        raise ValueError(f"codes is {codes.dtype}: {' or '.join(map(str, _CODES[format]))} is expected for this format")
     if kept[1:] != shape[1:]:
         raise ValueError(f"codes is {tuple(kept)}: {(kept[0],) + tuple(shape[1:])} is expected")
-    B, cols = shape[0], shape[-1]
-    return (B, S.numel() // max(B * cols, 1), cols, kept[0], _arg(S, "S", shape, _F32, dev), _arg(codes, "codes", kept, codes.dtype, dev),
+    B, cols, dev = shape[0], shape[-1], _device()
+    return (dev, B, S.numel() // max(B * cols, 1), cols, kept[0], _arg(S, "S", shape, _F32, dev), _arg(codes, "codes", kept, codes.dtype, dev),
             _arg(scales, "scales", kept[:-1], _F32, dev), None if slots is None else _arg(slots, "slots", shape[:1], _I32, dev))
 
 
 def darkattn_state_store(S, codes, scales, slots=None, format=STATE_I8, stream=None):
-    """Rows of S [B, ..., cols] into the 8-bit cache codes [n_slots, ..., cols], scales [n_slots, ...]."""
-    dev = _device()
-    B, rows, cols, n, S_, c_, sc_, sl_ = _state_args(S, codes, scales, slots, dev)
+    """Rows of S [B, ..., cols] into the 8-bit cache codes [n_slots, ..., cols], scales [n_slots, ...]. codes is int8 (STATE_I8) or
+    float8_e4m3fn (STATE_E4M3), or uint8."""
+    dev, B, rows, cols, n, S_, c_, sc_, sl_ = _state_args(S, codes, scales, slots, format)
     rc = lib.darkattn_state_store(B, rows, cols, S_, sl_, n, format, c_, sc_, _stream_of(stream, dev))
     if rc:
         _check(rc, "darkattn_state_store")
 
 
 def darkattn_state_load(codes, scales, S, slots=None, format=STATE_I8, stream=None):
-    """Rows of the 8-bit cache back into S [B, ..., cols]."""
-    dev = _device()
-    B, rows, cols, n, S_, c_, sc_, sl_ = _state_args(S, codes, scales, slots, dev)
+    """Rows of the 8-bit cache back into S [B, ..., cols]; codes as for the store."""
+    dev, B, rows, cols, n, S_, c_, sc_, sl_ = _state_args(S, codes, scales, slots, format)
     rc = lib.darkattn_state_load(B, rows, cols, c_, sc_, sl_, n, format, S_, _stream_of(stream, dev))
     if rc:
         _check(rc, "darkattn_state_load")
