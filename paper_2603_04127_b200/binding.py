@@ -366,6 +366,7 @@ def darkattn_decay_plan(B, H, N, d, *, dv=0, dtype=BF16, H_kv=0, path=PATH_AUTO,
 
 
 _F32, _I32 = torch.float32, torch.int32
+_MOST = 2 ** 31 - 1     # of what the library takes as int32: a larger count would wrap on its way there
 
 
 def _arg(t, name, shape, dtype, device):
@@ -429,7 +430,7 @@ def darkattn_decay_step(plan: DecayPlan, q, k, v, log_decay, S, o, slots=None, s
     pool = S.shape
     rc = lib.darkattn_decay_step(plan.handle, _arg(q, "q", qs, dt, dev), _arg(k, "k", ks, dt, dev), _arg(v, "v", vs, dt, dev),
                                  _arg(log_decay, "log_decay", plan._g, _F32, dev), _arg(S, "S", (pool[0],) + plan._s[1:] if pool else (), _F32, dev),
-                                 None if slots is None else _arg(slots, "slots", plan._n, _I32, dev), pool[0], _arg(o, "o", os_, dt, dev),
+                                 None if slots is None else _arg(slots, "slots", plan._n, _I32, dev), min(pool[0], _MOST), _arg(o, "o", os_, dt, dev),
                                  _stream_of(stream, dev))
     if rc:
         _check(rc, "darkattn_decay_step")
@@ -454,7 +455,8 @@ def _state_args(S, codes, scales, slots, format):
     if kept[1:] != shape[1:]:
         raise ValueError(f"codes is {tuple(kept)}: {(kept[0],) + tuple(shape[1:])} is expected")
     B, cols, dev = shape[0], shape[-1], _device()
-    return (dev, B, S.numel() // max(B * cols, 1), cols, kept[0], _arg(S, "S", shape, _F32, dev), _arg(codes, "codes", kept, codes.dtype, dev),
+    # (slots are int32 too: those behind _MOST cannot be named; B, rows and cols as large are refused by the library)
+    return (dev, min(B, _MOST), min(S.numel() // max(B * cols, 1), _MOST), min(cols, _MOST), min(kept[0], _MOST), _arg(S, "S", shape, _F32, dev), _arg(codes, "codes", kept, codes.dtype, dev),
             _arg(scales, "scales", kept[:-1], _F32, dev), None if slots is None else _arg(slots, "slots", shape[:1], _I32, dev))
 
 
