@@ -5,8 +5,6 @@
 // of the output, whose share of the state stays in shared memory for the whole segment.
 #include "decay.cuh"
 
-#include <float.h>
-
 namespace darkattn {
 namespace {
 

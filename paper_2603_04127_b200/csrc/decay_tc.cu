@@ -61,11 +61,6 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, const void 
     asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
                  ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z) : "memory");
 }
-template <int N> __device__ __forceinline__ void tmem_ld(uint32_t a, uint32_t (&v)[N])
-{
-    if constexpr (N == 32) tmem_ld32(a, v);
-    else tmem_ld16(a, v);
-}
 __device__ __forceinline__ float f(uint32_t x) { return __uint_as_float(x); }
 
 // Shared memory by its 32-bit addresses: all of a block's are one number, read once, and constants.
@@ -168,6 +163,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
 {
     using M = TcSmem<DY, DZ, MAIN>;
     constexpr int W = DZ / kGroups;                       // columns of O, D and the state a warp takes
+    static_assert(kGroups == 2 && (W == 32 || W == 64), "blocks of scores, tables and loads are laid out for two groups");
     // Narrow tiles (64 x 64): a state has half the rows of tensor memory. The tokens' two halves take one half of the rows each, so that all
     // warps transpose (with one half idle it was the longest step of a chunk), and leave two states, whose sum is the state: D is Y^T Z of the
     // first 64 tokens in its upper left quarter, of the others in its lower right one, and X S is [X X] times both.
@@ -575,14 +571,13 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 tc_fence_after();
                 const float keep = MAIN ? pw[L] : 1.f, share = behind;
                 if (!MAIN) behind *= pw[L];
-                constexpr int kLd = W < 32 ? W : 32;
 #pragma unroll
-                for (int h = 0; h < W; h += kLd) {
-                    uint32_t o[kLd];
-                    tmem_ld<kLd>(at + kD + half * 64 + z0 + h, o);
+                for (int h = 0; h < W; h += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(at + kD + half * 64 + z0 + h, o);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int j = 0; j < kLd; ++j) s[h + j] = MAIN ? fmaf(keep, s[h + j], f(o[j])) : fmaf(share, f(o[j]), s[h + j]);
+                    for (int j = 0; j < 32; ++j) s[h + j] = MAIN ? fmaf(keep, s[h + j], f(o[j])) : fmaf(share, f(o[j]), s[h + j]);
                 }
                 if (MAIN) put_state();
                 tc_fence_before();
@@ -592,26 +587,25 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
                 DWAIT(PZ + it % M::kStages, it / M::kStages & 1);
                 if (g == G - 1) {
                     tc_fence_after();
-                    constexpr int kLd = W < 32 ? W : 32;
                     const uint32_t stage = sbase + it % M::kStages * M::kStage + own;
 #pragma unroll
-                    for (int h = 0; h < W; h += kLd) {
-                        uint32_t o[kLd];
-                        tmem_ld<kLd>(at + kO + z0 + h, o);
+                    for (int h = 0; h < W; h += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(at + kO + z0 + h, o);
                         if (DZ == 64 && (has0 || k > 0)) {
-                            uint32_t x[kLd];
-                            tmem_ld<kLd>(at + kX + z0 + h, x);
+                            uint32_t x[32];
+                            tmem_ld32(at + kX + z0 + h, x);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int j = 0; j < kLd; ++j) o[j] = __float_as_uint(fmaf(f(x[j]), x_row, f(o[j])));
+                            for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(fmaf(f(x[j]), x_row, f(o[j])));
                         }
                         tmem_wait_ld();
-                        if (h + kLd == W) {
+                        if (h + 32 == W) {
                             tc_fence_before();
                             arrive_warp(bar + 8 * O_READ, lane);
                         }
 #pragma unroll
-                        for (int q = 0; q < kLd / 8; ++q) {
+                        for (int q = 0; q < 4; ++q) {
                             const uint4 r = pack8(o + 8 * q);
                             if (L == C) sts16(stage ^ ((h / 8 + q) << 4), r.x, r.y, r.z, r.w);
                             else if (row < L && z0 + h + 8 * q < c) *reinterpret_cast<uint4 *>(O + (size_t)(t0 + row) * c + z0 + h + 8 * q) = r;
