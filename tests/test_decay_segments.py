@@ -20,7 +20,7 @@ import math
 import pytest
 import torch
 
-from tests.test_decay import binding, blank_padding, check, dev, make, ops_of, oracle_backward, oracle_forward, poison_padding  # noqa: F401
+from tests.test_decay import SHAPES, binding, blank_padding, check, dev, make, ops_of, oracle_backward, oracle_forward, poison_padding  # noqa: F401
 
 C, FEW = 128, 32                                # a chunk of the tensor-core kernel; up to so many rows its scores are kept in two parts
 AGAINST_ROUNDED, AGAINST_EXACT = 1.15, 0.0032 * 1.05
@@ -319,3 +319,76 @@ def _compare(plan, binding, D, t, got, state, gradients):  # noqa: F811
             assert a <= 1 and b <= 1, f"{name}: {a:.3f} of the bound on the norm against the rounded form, {b:.3f} against the exact one"
     if state is not None:
         _within(state, want_state, mag_state, n, torch.float32, tensor, "state")
+
+
+# ------------------------------------------------------------------------------------------------ short calls without states, growing states, the most heads
+def _both_calls(binding, t, path, state_out):  # noqa: F811
+    B, H, N, d = t["q"].shape
+    Hk, dv = t["k"].shape[1], t["v"].shape[3]
+    plan = binding.darkattn_decay_plan(B, H, N, d, dv=dv, H_kv=Hk, dtype=binding.BF16 if t["q"].dtype == torch.bfloat16 else binding.F32, path=path)
+    D, ws = dev(t), plan.alloc_workspace()
+    O = torch.full((B, H, N, dv), 7.0, dtype=t["q"].dtype, device="cuda")
+    new = lambda x: torch.full_like(D[x], float("nan"))  # noqa: E731
+    grads = {"dq": new("q"), "dk": new("k"), "dv": new("v")}
+    S_out, dS_in = (torch.full((B, Hk, d, dv), float("nan"), device="cuda") if state_out else None for _ in range(2))
+    binding.darkattn_decay_forward(plan, D["q"], D["k"], D["v"], D["g"], O, ws, lengths=D["lengths"], S_in=D["S"], S_out=S_out)
+    assert binding.darkattn_decay_last_device_status(plan, ws) == binding.OK
+    _compare(plan, binding, D, t, {"o": O}, S_out, False)
+    binding.darkattn_decay_backward(plan, D["q"], D["k"], D["v"], D["g"], D["do"], *grads.values(), ws, lengths=D["lengths"], S_in=D["S"], dS_out=D["dS"], dS_in=dS_in)
+    assert binding.darkattn_decay_last_device_status(plan, ws) == binding.OK
+    _compare(plan, binding, D, t, grads, dS_in, True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_calls_without_states_out(binding, shape, dtype):  # noqa: F811
+    B, H, N, d, dv, Hk = shape
+    for path in (binding.PATH_SIMT, binding.PATH_AUTO):
+        for states_in in ((), ("S",), ("dS",), ("S", "dS")):
+            t = _inputs((B, H, N, d, dv, Hk, dtype, path), 80 + N, states_in, [N // 2, N] if len(states_in) == 1 else None)
+            _both_calls(binding, t, path, False)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,dv", [(64, 64), (128, 72)])
+def test_states_that_grow(binding, dtype, d, dv):  # noqa: F811
+    """A decay above 1 is not refused."""
+    for path in (binding.PATH_SIMT, binding.PATH_AUTO):
+        for state_out in (False, True):
+            _both_calls(binding, make(2, 4, 600, d, dv, 2, dtype, seed=90, decays=(0.004, 0.02)), path, state_out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_as_many_heads_as_there_may_be(binding, dtype):  # noqa: F811
+    """65535 of them: prompts, gradients, a step, a cache, whose last head is what it is by itself."""
+    H, N, d = 65535, 3, 8
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rnd = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    kind = binding.BF16 if dtype == "bf16" else binding.F32
+    q, k, v, do = (rnd(1, H, N, d).to(dt) for _ in range(4))
+    S, g = rnd(1, H, d, d), -rnd(H).abs()
+
+    def calls(*at):
+        x = [t[:, at].contiguous() if at else t for t in (q, k, v, do, S)]
+        decay = g[list(at)].contiguous() if at else g
+        h = x[0].shape[1]
+        plan, one = (binding.darkattn_decay_plan(1, h, n, d, dtype=kind) for n in (N, 1))
+        ws = plan.alloc_workspace()
+        O, S_out, dS_in = torch.empty_like(x[2]), torch.empty_like(x[4]), torch.empty_like(x[4])
+        binding.darkattn_decay_forward(plan, *x[:3], decay, O, ws, S_in=x[4], S_out=S_out)
+        grads = [torch.empty_like(y) for y in x[:3]]
+        binding.darkattn_decay_backward(plan, *x[:3], decay, x[3], *grads, ws, S_in=x[4], dS_in=dS_in)
+        pool, o = S_out.clone(), torch.empty_like(x[0][:, :, 0]).contiguous()
+        binding.darkattn_decay_step(one, *(y[:, :, 0].contiguous() for y in x[:3]), decay, pool, o)
+        kept = pool.reshape(h, 1, d, d)
+        codes, scales, back = torch.empty(h, 1, d, d, dtype=torch.int8, device="cuda"), torch.empty(h, 1, d, device="cuda"), torch.empty_like(kept)
+        binding.darkattn_state_store(kept, codes, scales)
+        binding.darkattn_state_load(codes, scales, back)
+        return [O, S_out, dS_in, *grads, pool, o[:, :, None], back.reshape(1, h, d, d)]
+
+    for whole, part in zip(calls(), calls(0, 40000, 65534)):
+        assert torch.equal(whole[:, [0, 40000, 65534]], part)
