@@ -430,7 +430,7 @@ def darkattn_decay_step(plan: DecayPlan, q, k, v, log_decay, S, o, slots=None, s
     pool = S.shape
     rc = lib.darkattn_decay_step(plan.handle, _arg(q, "q", qs, dt, dev), _arg(k, "k", ks, dt, dev), _arg(v, "v", vs, dt, dev),
                                  _arg(log_decay, "log_decay", plan._g, _F32, dev), _arg(S, "S", (pool[0],) + plan._s[1:] if pool else (), _F32, dev),
-                                 None if slots is None else _arg(slots, "slots", plan._n, _I32, dev), min(pool[0], _MOST), _arg(o, "o", os_, dt, dev),
+                                 None if slots is None else _arg(slots, "slots", plan._n, _I32, dev), pool[0] if pool[0] <= _MOST else _MOST, _arg(o, "o", os_, dt, dev),
                                  _stream_of(stream, dev))
     if rc:
         _check(rc, "darkattn_decay_step")
@@ -450,13 +450,16 @@ def _state_args(S, codes, scales, slots, format):
     shape, kept = S.shape, codes.shape
     if len(shape) < 2 or len(kept) != len(shape) or codes.element_size() != 1:
         raise ValueError("S is [B, ..., cols], codes one byte an element [n_slots, ..., cols]")
-    if codes.dtype not in _CODES.get(format, (codes.dtype,)):        # (an unknown format is the library's to refuse)
-        raise ValueError(f"codes is {codes.dtype}: {' or '.join(map(str, _CODES[format]))} is expected for this format")
+    own = _CODES.get(format)                                 # (an unknown format is the library's to refuse)
+    if own is not None and codes.dtype not in own:
+        raise ValueError(f"codes is {codes.dtype}: {' or '.join(map(str, own))} is expected for this format")
     if kept[1:] != shape[1:]:
         raise ValueError(f"codes is {tuple(kept)}: {(kept[0],) + tuple(shape[1:])} is expected")
-    B, cols, dev = shape[0], shape[-1], _device()
-    # (slots are int32 too: those behind _MOST cannot be named; B, rows and cols as large are refused by the library)
-    return (dev, min(B, _MOST), min(S.numel() // max(B * cols, 1), _MOST), min(cols, _MOST), min(kept[0], _MOST), _arg(S, "S", shape, _F32, dev), _arg(codes, "codes", kept, codes.dtype, dev),
+    B, cols, n, size, dev = shape[0], shape[-1], kept[0], S.numel(), _device()
+    rows = size // max(B * cols, 1)
+    if size > _MOST or n > _MOST:       # (slots are int32 too: those behind _MOST cannot be named; B, rows and cols as large are refused by the library)
+        B, rows, cols, n = (min(x, _MOST) for x in (B, rows, cols, n))
+    return (dev, B, rows, cols, n, _arg(S, "S", shape, _F32, dev), _arg(codes, "codes", kept, codes.dtype, dev),
             _arg(scales, "scales", kept[:-1], _F32, dev), None if slots is None else _arg(slots, "slots", shape[:1], _I32, dev))
 
 
