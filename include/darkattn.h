@@ -239,6 +239,12 @@ darkattn_status_t darkattn_forward_static(darkattn_plan_t plan, const void *Q, c
  *                                  them are padding: never used, whatever they hold. Rows of O behind the end are left as
  *                                  they were, those of dQ, dK and dV are set to zero.
  *
+ * Roundings. Sums and running states are FP32. SIMT: rows of bf16 tensors are rounded as they are stored and nowhere else. TENSOR (what AUTO takes for
+ * bf16 of these widths): beside that masked scores times their decays, and the state as rows read it, are rounded to bf16, once each
+ * (scores of chunks of up to 32 rows are kept to 16 bits), and what a token adds to the state to 16 bits, to 24 where the state is asked for (S_out, dS_in,
+ * which are FP32 results). Rows come out off by 0.0024 of their norm where their own rounding is 0.0017. Their last bits depend on
+ * whether S_out (for dK and dV: dS_in) is asked for, and on how the plan cuts sequences; two calls with the same arguments agree in every bit.
+ *
  * Conventions as at the top of this file (contiguous, 16-byte aligned - log_decay, lengths and slots 4 -, caller-owned,
  * asynchronous on the stream, nothing allocated). Inputs have to be finite: what is not spreads to its whole chunk. What a call writes
  * must overlap nothing else that it reads or writes (DARKATTN_ERR_INVALID_ARG). Calls whose GPU work may run at the same time

@@ -314,7 +314,7 @@ __global__ void __launch_bounds__(kThreadsS, R <= 5 ? 2 : 1) decay_tile_kernel(c
 
 // ---------------------------------------------------------------- wider
 // What the tiles above are, by slices of 64 of X and Y and for 64 columns of Z; the scores are formed again for each 64 columns. Bound by the products and
-// the barriers between them: 4 x 16 heads of 2048 tokens, 256 x 256, 2.5 ms (0.9 by their arithmetic alone).
+// the barriers between them: 4 x 16 heads of 2048 tokens, 256 x 256, 2.4 ms (0.9 by their arithmetic alone).
 struct SimtSmem {
     static constexpr int XT = 0, YT = XT + F * kPad, Yr = YT + F * kPad, Z = Yr + C * F, PT = Z + C * F, pw = PT + C * kPad, S = pw + 72;
     static int bytes(int a) { return (S + (a + F - 1) / F * F * F) * 4; }

@@ -4,8 +4,8 @@
 // Bound by the state, read and written once. A block takes CT columns of one head's state: its warps take rows in turn, every lane
 // four columns of a row; the products with the queries are summed over a thread's rows in registers, over the block's in shared memory.
 // The block's whole share of the state is on its way into shared memory before anything else happens (every thread copies what it will use
-// itself, so nothing is waited for but a thread's own copies): 128 sequences of 16 heads, 128 x 128 (268 MB to and fro) 44.9 us, 6.0 TB/s, at 64
-// columns a block; 45.9 at 32, 48.8 at 128; with loads into registers 52.4. 4 sequences: 3.2 us.
+// itself, so nothing is waited for but a thread's own copies): 128 sequences of 16 heads, 128 x 128 (268 MB to and fro) 47.2 us, 5.7 TB/s, over pools by
+// turns. On one pool, in part in L2, 43 to 45 at 64 columns a block, 46 at 32, 49 at 128; with loads into registers 52. 4 sequences: 3.2 us.
 #include "decay.cuh"
 
 namespace darkattn {

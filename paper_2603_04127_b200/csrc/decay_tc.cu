@@ -9,12 +9,12 @@
 // The state itself stays in the registers of eight warps in fp32, S <- lambda^L S + D; the rows read a copy rounded to bf16 (as P is
 // rounded: half a step of each term, like the rounding of the rows out: together 1.4 times the error of that rounding alone).
 // Everything moves by TMA, two to four chunks of X, Y and Z deep; the rows out are staged in the chunk's own tiles (stored from registers, 32 bytes a
-// thread, d 128 took 226 us for 212).
+// thread, d 128 took 7 % longer).
 //
 // What bounds it: shared memory. At width 128 a chunk's tiles, operands and copies are 3.8 thousand cycles of its 128 bytes a cycle (the products
 // by themselves 2.6), a chunk takes 4.5 thousand; at 64 2.3 of 3.4 thousand, the rest latencies of steps that wait for one another: scores
 // into P 500, the state 250 to 600, rows out 400, transposition 1100. (Warps of their own for some of the steps, 18 to 28 in all, overlap
-// them and made nothing faster: d 128 219 -> 275 us.) 4 x 37 heads of 8192 tokens, one block an SM: d 128 1.24 GB in 215 us, 5.8 TB/s; d 64 0.62 GB in 126, 4.9.
+// them and made nothing faster: d 128 219 -> 275 us.) 4 x 37 heads of 8192 tokens, one block an SM: d 128 1.24 GB in 218 us, 5.7 TB/s; d 64 0.62 GB in 126 to 145, 4.3 to 4.9.
 #include "decay.cuh"
 #include "tc_common.cuh"
 
@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kBlock, 1) decay_tc_kernel(const __grid_consta
     tc_fence_after();
     pdl_wait_tma();
     const uint32_t tmem = uniform(*tmem_slot);
-    // (The first block to start clears the status; a wait gives up milliseconds later.)
+    // (The first block to start clears the status; a wait gives up a second or two later.)
     if (A.clear && blockIdx.x == 0 && tid == 0) *A.status = 0;
 
     const int b = head / HX, hx = head % HX, hs = hx / (HX / A.Hkv);
@@ -721,11 +721,12 @@ bool decay_tc_supported(const darkattn_decay_desc_t &ds)
 // Segments, and the pieces whose states are summed first: the cheapest by an estimate in us, fitted to measurements on a B200. A chunk takes 2.6 us
 // (wide tiles, 64 to 128 columns) or 1.7 us while few blocks run, and what the memory gives when all SMs do (5.7 and, power-bound, 4.8 TB/s);
 // a chunk of the states alone 1.4 or 1.0 us, a wave of blocks 2 us more; two kernels more 9 or 4 us, twice that where there are two sets of states. One head of 8192 tokens, d 128: 178 us in one
-// segment, 31 in 32; 4 x 16 heads: 164 in one, 139 in two with two pieces each, 188 in four; 8 heads of 65536, d 64: 113 in 18.
-// Segments have to promise 8 % (a backward pass in one segment shares more of its reads in L2 than the estimate knows: 4 x 16 heads, 337 us
-// in one, 359 in two).
+// segment, 22.4 in 32, 24.5 in the 64 that it picks; 4 x 16 heads on one set of inputs, in part in L2 (on several by turns): 195 (167) in one, 141 (161 to 166)
+// in two with two pieces each, 165 (178) in two whole ones, 205 (194) in four; 8 heads of 65536, d 64: 920 in one, 105 in 18.
+// Segments have to promise 8 % (a backward pass in one segment shares more of its reads in L2 than the estimate knows: 4 x 16 heads, 382 us
+// in one, 424 in two).
 // `heads` heads of a pass take an item a chunk, `sums` of them G: those that sum over a group's heads. Where these are the longer ones nothing is done
-// before they are: 2 x 12 heads on 3, 898 tokens, gradients at d 96, dv 64: 129 us in one segment, 48 in several.
+// before they are: 2 x 12 heads on 3, 898 tokens, gradients at d 96, dv 64: 70 us in one segment, 39 in four.
 static void pick(int T, int d, int dv, DecayLoad rows, DecayLoad states, int sets, int &nseg, int &cps, int &sub)
 {
     const bool wide = d > 64 || dv > 64;
